@@ -317,6 +317,127 @@ epic_status epic_diag_lds_stream(int32_t blocks, int32_t threads, int32_t iters,
  * runtime reports them), for epic_diag_lds_stream's tick counts. */
 epic_status epic_diag_clock_rates(int32_t* shader_khz, int32_t* wall_khz);
 
+/* ---- What comes before and around the check: logits rows ----------------
+ *
+ * A denoiser answers with logits.  The three operators below make proposals of
+ * them (epic_sample, epic_propose) and train the denoiser on a teacher's
+ * (epic_distill_*).  They need no context: they know nothing of the grammar.
+ *
+ * Rows.  Row (b, i), 0 <= b < batch and 0 <= i < rows, holds the `vocab` logits
+ * of sequence b at position start[b] + i of its n tokens, elements
+ * data[b*seq_stride + i*row_stride + 0 .. vocab): a window of `rows` positions
+ * per sequence (the active block in block decoding).  d_start (int32 [batch])
+ * NULL: every window starts at position 0.  A row counts when its position is
+ * inside the sequence and masked there (d_seqs int32 [batch*n], -1 = MASK);
+ * with d_seqs NULL (then n and d_start are not read) every row counts.  Rows
+ * that do not count are not read: they may hold anything.
+ *
+ * data is a device pointer aligned to its element; rows need no more alignment
+ * and no particular stride (a stride of 0 repeats a row; the rows of a gradient
+ * must not overlap).  1 <= vocab <= 262144, else EPIC_ERR_UNSUPPORTED; offsets
+ * are 64-bit.  batch * rows = 0 is no error.  The calls allocate nothing, keep
+ * nothing and may be captured in a HIP graph; the same inputs give the same
+ * bits, whatever else is in the batch. */
+typedef enum { EPIC_F32 = 0, EPIC_F16 = 1, EPIC_BF16 = 2 } epic_dtype;
+
+typedef struct {
+  void* data;        /* device */
+  int32_t dtype;     /* epic_dtype */
+  int32_t batch;     /* sequences */
+  int32_t rows;      /* rows per sequence */
+  int32_t vocab;     /* logits per row */
+  int64_t seq_stride; /* elements from a sequence's first row to the next's */
+  int64_t row_stride; /* elements from a row to the next of its sequence */
+} epic_rows_desc;
+
+/* Sampling with temperature, top-k, top-p and min-p from given uniform
+ * numbers: one token and its confidence for every row that counts.
+ *
+ * With M the row's largest logit and T its temperature, token t has
+ *   x_t = (l_t - M) * c,  c = log2(e) / T rounded to float32,  e_t = 2^x_t,
+ *   w_t = floor(2^31 * e_t + 1/2),  a whole number; W = sum of all w_t
+ * (x, e and the sum with 1/2 in float32).  Sums of whole numbers depend on no order, so neither does the token drawn.
+ * NaN and -inf logits have w = 0 and are never drawn.
+ * Tokens are ordered by descending logit, ties to the lower id.  Kept are the
+ * tokens that pass all of
+ *   top-k (k > 0):   the first k; S their mass (else S = W);
+ *   top-p (p < 1):   the shortest prefix whose mass is at least
+ *                    max(1, floor(S * floor(2^24 p) / 2^24)), p <= 0: the first;
+ *   min-p (q > 0):   w_t >= floor(2^31 q + 1/2), q capped at 1.
+ * With D the mass kept and U = floor(2^24 u), u the row's uniform number
+ * (capped to [0, 1 - 2^-24], NaN: 0), the token is the lowest id at which the
+ * kept mass up to it exceeds floor(D * U / 2^24).  Its confidence is
+ * 2^31 e_t / W: its probability at that temperature before the filters.
+ * T <= 0 is greedy: the first of the order, with its probability at T = 1.
+ *
+ * d_uniform: float32 [batch*rows].  Settings per sequence, NULL for the default:
+ * d_temperature float32 [batch] (1), d_top_k int32 (off), d_top_p float32
+ * (off), d_min_p float32 (off); NaN in top-p or min-p means off.
+ * d_tok int32 [batch*rows], d_conf float32 [batch*rows]: -1 and 0 for a row
+ * that does not count, has no finite logit, has a logit of +inf or a NaN
+ * temperature.  A mask of the type's lowest finite value is a finite logit:
+ * beside an ordinary one its weight is 0, a row of nothing else is uniform. */
+epic_status epic_sample(const epic_rows_desc* logits, const int32_t* d_seqs, int32_t n, const int32_t* d_start,
+                        const float* d_uniform, const float* d_temperature, const int32_t* d_top_k,
+                        const float* d_top_p, const float* d_min_p, int32_t* d_tok, float* d_conf,
+                        hipStream_t stream);
+
+/* Proposals of a step from sampled tokens: of each sequence the per_seq most
+ * confident rows (float32, descending, ties to the lower row) that have a
+ * token, as the candidate arrays that epic_validate_batch,
+ * epic_select_compatible and epic_commit_fallback read.
+ * d_tok int32 and d_conf float32 [batch*rows] as epic_sample writes them; a
+ * row with a token below 0 or a NaN confidence is no proposal.  d_start as
+ * above, or NULL.  1 <= per_seq <= 64 (what selection takes of a sequence).
+ * Sequence b's candidates are d_cand_*[d_offsets[b] .. d_offsets[b+1]), most
+ * confident first, position = d_start[b] + row; d_offsets int32 [batch+1]
+ * starts at 0, and d_offsets[batch] is the C of the calls that follow.  The
+ * arrays hold batch*per_seq entries; those past the last candidate are set to
+ * -1 (confidence 0). */
+epic_status epic_propose(const int32_t* d_tok, const float* d_conf, int32_t batch, int32_t rows,
+                         const int32_t* d_start, int32_t per_seq, int32_t* d_cand_seq, int32_t* d_cand_pos,
+                         int32_t* d_cand_tok, float* d_cand_conf, int32_t* d_offsets, hipStream_t stream);
+
+/* Distillation from a teacher's top logits: the divergence of the student's
+ * rows from the teacher, which is known by K entries (id, logit) per row.
+ * With z = l / tau the student's scaled logits, S the set of the row's listed
+ * ids and t_k the teacher's logits:
+ *   with d_teacher_lse (float32 [batch*rows], the teacher's logsumexp of t /
+ *   tau over its whole vocabulary): q_k = exp(t_k/tau - lse_T), and
+ *   q_rest = max(0, 1 - sum q_k) is what the teacher leaves to the rest;
+ *   without (NULL): q = softmax of t / tau over the entries, q_rest = 0.
+ *   lse_rest = log sum_{j not in S} exp(z_j), lse = log sum_j exp(z_j),
+ *   p = exp(z - lse), p_rest = exp(lse_rest - lse),
+ *   loss = tau^2 (sum_k q_k (log q_k - log p_k) + q_rest (log q_rest - log p_rest)),
+ *   d loss / d l_j = tau (p_j - q_j) for j in S (q_j: the sum of j's entries),
+ *                    tau exp(z_j - lse_rest) (p_rest - q_rest) for the others.
+ * An entry with a negative id is absent; an entry of logit -inf is listed with
+ * q = 0.  When every finite logit of the row is listed, q_rest counts as 0.  A
+ * row that does not count, has no finite student logit or no entry (without
+ * d_teacher_lse: no entry above -inf) has loss 0 and gradient 0; an id >= vocab
+ * gives loss NaN and gradient 0.  NaN and +inf elsewhere give NaN.
+ *
+ * d_top_idx int32 and d_top_logit float32 [batch*rows*K], 1 <= K <= 1024, ids
+ * in any order; 0 < tau < inf.  d_loss float32 [batch*rows].  d_stats float32
+ * [batch*rows*2] receives lse and lse_rest of each row for the backward pass.
+ * Gradients: grad (its data, of the logits' type and shape, strides of its
+ * own, rounded to nearest even from float32) receives weight[row] times the
+ * derivative above for every row (0 in rows that do not count); it may be the
+ * logits themselves (the same data and strides), but not otherwise overlap
+ * them.  d_weight float32 [batch*rows]: the upstream gradient of each row's
+ * loss (NULL: 1).
+ * epic_distill_forward writes losses and stats and, when grad is not NULL, the
+ * gradient with one reading of the logits.  epic_distill_backward writes the
+ * gradient from the stats of an earlier forward pass over the same inputs. */
+epic_status epic_distill_forward(const epic_rows_desc* logits, const int32_t* d_seqs, int32_t n,
+                                 const int32_t* d_start, const int32_t* d_top_idx, const float* d_top_logit, int32_t K,
+                                 const float* d_teacher_lse, float tau, float* d_loss, float* d_stats,
+                                 const float* d_weight, const epic_rows_desc* grad, hipStream_t stream);
+epic_status epic_distill_backward(const epic_rows_desc* logits, const int32_t* d_seqs, int32_t n,
+                                  const int32_t* d_start, const int32_t* d_top_idx, const float* d_top_logit,
+                                  int32_t K, const float* d_teacher_lse, float tau, const float* d_stats,
+                                  const float* d_weight, const epic_rows_desc* grad, hipStream_t stream);
+
 const char* epic_status_string(epic_status s);
 
 #ifdef __cplusplus

@@ -29,6 +29,7 @@ FUNCTIONS = ["epic_ctx_create", "epic_ctx_destroy", "epic_workspace_bytes", "epi
              "epic_ctx_device_error", "epic_ctx_work_counters", "epic_ctx_set_timing",
              "epic_ctx_set_witness_lds", "epic_ctx_kernel_stats",
              "epic_witness_workspace_bytes", "epic_witness",
+             "epic_sample", "epic_propose", "epic_distill_forward", "epic_distill_backward",
              "epic_diag_lds_stream", "epic_diag_clock_rates", "epic_status_string"]
 KERNEL_KINDS = ["lexmemo", "base", "validate", "select", "fallback", "spec_bookkeeping", "spec_unused"]
 
@@ -51,6 +52,12 @@ class _Grammar(ctypes.Structure):
 
 class _Vocab(ctypes.Structure):
     _fields_ = [("vocab_size", ctypes.c_int32), ("bytes", ctypes.c_void_p), ("offsets", ctypes.c_void_p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("seq_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -99,6 +106,15 @@ def lib() -> ctypes.CDLL:
         L.epic_witness_workspace_bytes.restype = sz
         L.epic_witness.argtypes = [P, P, i32, i32, P, i32, P, i32, P, P, sz, P, sz, P]
         L.epic_witness.restype = ctypes.c_int
+        rows, f32 = ctypes.POINTER(_Rows), ctypes.c_float
+        L.epic_sample.argtypes = [rows, P, i32] + [P] * 9
+        L.epic_sample.restype = ctypes.c_int
+        L.epic_propose.argtypes = [P, P, i32, i32, P, i32] + [P] * 6
+        L.epic_propose.restype = ctypes.c_int
+        L.epic_distill_forward.argtypes = [rows, P, i32, P, P, P, i32, P, f32, P, P, P, rows, P]
+        L.epic_distill_forward.restype = ctypes.c_int
+        L.epic_distill_backward.argtypes = [rows, P, i32, P, P, P, i32, P, f32, P, P, rows, P]
+        L.epic_distill_backward.restype = ctypes.c_int
         L.epic_diag_lds_stream.argtypes = [i32, i32, i32, P, P]
         L.epic_diag_lds_stream.restype = ctypes.c_int
         L.epic_diag_clock_rates.argtypes = [ctypes.POINTER(i32), ctypes.POINTER(i32)]
@@ -291,3 +307,146 @@ def clock_rates() -> tuple:
     a, b = ctypes.c_int32(0), ctypes.c_int32(0)
     _check("epic_diag_clock_rates", lib().epic_diag_clock_rates(ctypes.byref(a), ctypes.byref(b)))
     return int(a.value), int(b.value)
+
+
+# ---------------------------------------------------------------------------
+# Logits rows: what comes before and around the check.  Logits are a tensor
+# [B, m, V] (float32, float16 or bfloat16, any strides with V's 1): row i of
+# sequence b is its position start[b] + i of the n tokens in `seqs`.  Outputs
+# are the caller's tensors.  A tensor of the wrong type, shape or device is a
+# ValueError; what the library refuses is an EpicError.
+
+_DTYPES: dict = {}
+
+
+def _dtypes() -> dict:
+    if not _DTYPES:
+        import torch
+
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+        _DTYPES.update(i32=torch.int32, f32=torch.float32)
+    return _DTYPES
+
+
+def _rows(name, t, device=None) -> _Rows:
+    if t.dim() != 3 or t.dtype not in _dtypes():
+        raise ValueError(f"{name}: a [B, m, V] tensor of float32, float16 or bfloat16, got {tuple(t.shape)} {t.dtype}")
+    B, m, V = t.shape
+    sb, sm, sv = t.stride()
+    if sv != 1 and V > 1:
+        raise ValueError(f"{name}: a row's logits have to be adjacent, got strides {t.stride()}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name}: on {t.device}, needs a GPU tensor" + (f" on {device}" if device else ""))
+    return _Rows(t.data_ptr(), _DTYPES[t.dtype], B, m, V, sb, sm)
+
+
+def _arg(name, t, dtype, shape, device):
+    """The address of a contiguous tensor of that type and shape (None: 0)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
+                         + ("" if t.is_contiguous() else ", not contiguous"))
+    return t.data_ptr()
+
+
+def _window(seqs, start, B, device):
+    """Addresses of the sequences and the windows' first positions, and n."""
+    i32 = _DTYPES["i32"]
+    if seqs is None:
+        return 0, 0, 0  # every row counts
+    if seqs.dim() != 2:
+        raise ValueError(f"seqs: int32 [B, n], got {tuple(seqs.shape)}")
+    n = seqs.shape[1]
+    return _arg("seqs", seqs, i32, (B, n), device), n, _arg("start", start, i32, (B,), device)
+
+
+def _call(fn, device, stream, *args):
+    """The library call on `stream` (default: the device's current one), with
+    the tensors' device current."""
+    import torch
+
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if torch.cuda.current_device() == device.index:
+        _check(fn, getattr(lib(), fn)(*args, s.cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn, getattr(lib(), fn)(*args, s.cuda_stream))
+
+
+def sample(logits, seqs, uniform, tok, conf, start=None, temperature=None, top_k=None, top_p=None, min_p=None,
+           stream=None):
+    """epic_sample: a token and its confidence for every masked row.  seqs int32
+    [B, n] or None (every row counts), uniform float32 [B, m]; tok int32 and
+    conf float32 [B, m] are written.  Settings per sequence, or None:
+    temperature, top_p, min_p float32 [B], top_k int32 [B]; start int32 [B]."""
+    rows = _rows("logits", logits)
+    dev, (B, m, _) = logits.device, logits.shape
+    i32, f32 = _DTYPES["i32"], _DTYPES["f32"]
+    sp, n, st = _window(seqs, start, B, dev)
+    if uniform is None or tok is None or conf is None:
+        raise ValueError("uniform, tok and conf are needed")
+    _call("epic_sample", dev, stream, ctypes.byref(rows), sp, n, st, _arg("uniform", uniform, f32, (B, m), dev),
+          _arg("temperature", temperature, f32, (B,), dev), _arg("top_k", top_k, i32, (B,), dev),
+          _arg("top_p", top_p, f32, (B,), dev), _arg("min_p", min_p, f32, (B,), dev),
+          _arg("tok", tok, i32, (B, m), dev), _arg("conf", conf, f32, (B, m), dev))
+
+
+def propose(tok, conf, per_seq, cand_seq, cand_pos, cand_tok, cand_conf, offsets, start=None, stream=None):
+    """epic_propose: the per_seq most confident tokens of every sequence as the
+    candidate arrays of validate, select and fallback (int32 [B*per_seq] each,
+    cand_conf float32), and offsets int32 [B + 1]: sequence b's candidates are
+    offsets[b] to offsets[b+1]."""
+    _dtypes()
+    i32, f32 = _DTYPES["i32"], _DTYPES["f32"]
+    if tok.dim() != 2 or not tok.is_cuda:
+        raise ValueError(f"tok: int32 [B, m] on a GPU, got {tuple(tok.shape)} on {tok.device}")
+    dev, (B, m) = tok.device, tok.shape
+    C = (B * per_seq,)
+    _call("epic_propose", dev, stream, _arg("tok", tok, i32, (B, m), dev), _arg("conf", conf, f32, (B, m), dev), B, m,
+          _arg("start", start, i32, (B,), dev), per_seq, _arg("cand_seq", cand_seq, i32, C, dev),
+          _arg("cand_pos", cand_pos, i32, C, dev), _arg("cand_tok", cand_tok, i32, C, dev),
+          _arg("cand_conf", cand_conf, f32, C, dev), _arg("offsets", offsets, i32, (B + 1,), dev))
+
+
+def _teacher(logits, top_idx, top_logit, teacher_lse):
+    dev, (B, m, _) = logits.device, logits.shape
+    if top_idx.dim() != 3:
+        raise ValueError(f"top_idx: int32 [B, m, K], got {tuple(top_idx.shape)}")
+    K = top_idx.shape[2]
+    return (_arg("top_idx", top_idx, _DTYPES["i32"], (B, m, K), dev),
+            _arg("top_logit", top_logit, _DTYPES["f32"], (B, m, K), dev), K,
+            _arg("teacher_lse", teacher_lse, _DTYPES["f32"], (B, m), dev))
+
+
+def distill_forward(logits, seqs, top_idx, top_logit, loss, stats, start=None, teacher_lse=None, tau=1.0, weight=None,
+                    grad=None, stream=None):
+    """epic_distill_forward: per row the divergence of softmax(logits / tau)
+    from the teacher's top_logit float32 at top_idx int32 [B, m, K] (with
+    teacher_lse float32 [B, m] also of what the teacher leaves to the other
+    tokens) into loss float32 [B, m], and stats float32 [B, m, 2] for the
+    backward pass; with grad (like logits, or logits itself) also the gradient
+    of sum(weight * loss), weight float32 [B, m] or None for 1."""
+    rows = _rows("logits", logits)
+    dev, (B, m, _) = logits.device, logits.shape
+    f32 = _DTYPES["f32"]
+    sp, n, st = _window(seqs, start, B, dev)
+    ti, tl, K, te = _teacher(logits, top_idx, top_logit, teacher_lse)
+    g = None if grad is None else ctypes.byref(_rows("grad", grad, dev))
+    _call("epic_distill_forward", dev, stream, ctypes.byref(rows), sp, n, st, ti, tl, K, te, tau,
+          _arg("loss", loss, f32, (B, m), dev), _arg("stats", stats, f32, (B, m, 2), dev),
+          _arg("weight", weight, f32, (B, m), dev), g)
+
+
+def distill_backward(logits, seqs, top_idx, top_logit, stats, weight, grad, start=None, teacher_lse=None, tau=1.0,
+                     stream=None):
+    """epic_distill_backward: the gradient of sum(weight * loss) from the stats
+    of a distill_forward over the same inputs."""
+    rows = _rows("logits", logits)
+    dev, (B, m, _) = logits.device, logits.shape
+    f32 = _DTYPES["f32"]
+    sp, n, st = _window(seqs, start, B, dev)
+    ti, tl, K, te = _teacher(logits, top_idx, top_logit, teacher_lse)
+    _call("epic_distill_backward", dev, stream, ctypes.byref(rows), sp, n, st, ti, tl, K, te, tau,
+          _arg("stats", stats, f32, (B, m, 2), dev), _arg("weight", weight, f32, (B, m), dev),
+          ctypes.byref(_rows("grad", grad, dev)))
