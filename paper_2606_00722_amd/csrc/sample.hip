@@ -7,21 +7,25 @@ namespace epic_rows {
 //
 // One workgroup per row.  The row is read once into registers, J vectors a
 // lane (J = 0, rows too long for that: every pass reads it again).  Two passes
-// over the registers give the largest logit and the weights' sum W.
+// over the registers give the largest logit and the weights' sum W; without a
+// filter one wavefront then finds the token.
 //
-// Without a filter, one wavefront then finds the token.  With top-k or top-p
-// the tokens that can matter are few in most rows: those above a bound that
-// follows from the largest logits of the lanes (top-k), or from the mass that
-// top-p leaves out (a token below (1 - p) W / V cannot be needed).  If there
-// are at most kList of them they go into LDS in the order of their ids, are
-// sorted by logit, and everything else happens there.  If there are more (flat
-// rows), the threshold is found by rounds of a histogram over the row, which
-// is read again from L2 by every round.
+// With a filter the tokens that it can keep are few in most rows, and end in a
+// list in LDS in the order of their ids, where one wavefront does the rest:
+//  * top-k: those above a bound that follows from the lanes' largest logits;
+//  * top-p: a histogram of the weights over the logits gives the step in which
+//    the mass is reached, and those up to that step are listed;
+//  * min-p: those above the logit that it stands for.
+// If the list is too short for them (flat rows), only the tokens of that step
+// are listed; they give the exact border, and one more pass sums what is kept.
+// If even those are too many (thousands of equal logits), the border is found
+// by rounds of ever finer histograms.  The passes after the first two read the
+// row again, from L2: as unrolled code over registers they took as many
+// registers as there are, and their arithmetic costs seven times the reading.
 //
 // Weights are whole numbers (2^31 for the likeliest token), so the order of
 // the sums, the atomics' order among them, changes no result.
 constexpr float kOne = 2147483648.0f;
-constexpr int kBins = 1024;
 
 struct SampleArgs {
   const char* data;
@@ -46,15 +50,15 @@ EPIC_DEV uint32_t to_u32(float f) {
   return r;
 }
 
-// The weight of a logit: the two roundings of (l - M) * c are part of its
-// definition, so they may not be contracted into one.
-EPIC_DEV float power(float l, float M, float c) {
-  return __builtin_amdgcn_exp2f(__fmul_rn(__fsub_rn(l, M), c));
+// The exponent of a logit: its two roundings are part of the definition, so
+// they may not be contracted into one.  Monotonic, and so are the steps that
+// are counted of it.
+EPIC_DEV float exponent(float l, float M, float c) { return __fmul_rn(__fsub_rn(l, M), c); }
+EPIC_DEV float power(float l, float M, float c) { return __builtin_amdgcn_exp2f(exponent(l, M, c)); }
+EPIC_DEV uint32_t weight_of(float x) {
+  return to_u32(__builtin_fmaf(__builtin_amdgcn_exp2f(x), kOne, 0.5f));  // 2^31 e is exact: one rounding either way
 }
-EPIC_DEV uint32_t weight(float l, float M, float c) {
-  return to_u32(__builtin_fmaf(power(l, M, c), kOne, 0.5f));  // 2^31 e is exact: one rounding either way
-}
-
+EPIC_DEV uint32_t weight(float l, float M, float c) { return weight_of(exponent(l, M, c)); }
 // Ordered keys: the logits' own bits as whole numbers in the order of the
 // values, 0.0 and -0.0 the same.
 template <int DT>
@@ -77,8 +81,8 @@ EPIC_DEV float of_key(uint32_t k) {
 template <int DT>
 constexpr float kLowest = DT == EPIC_F16 ? -65504.f : -3.38e38f;
 
-// A row read from memory by every pass; wavefronts have the same ids as the
-// lanes that hold it in registers.
+// A row read from memory by a pass; wavefronts have the same ids as the lanes
+// that hold it in registers.
 template <int DT>
 struct Row {
   const char* base;
@@ -86,49 +90,77 @@ struct Row {
 
   // id of element 0 of the lane's vector j
   EPIC_DEV int id(int j) const { return (first + j * 64 + lane) * kPer<DT>; }
-  EPIC_DEV Vec load(int j) const { return load_vec<DT>(base, first + j * 64 + lane, V); }
-  template <class F>
-  EPIC_DEV void elements(F&& f) const {
+  EPIC_DEV Vec load(int j) const {
+    const int at = first + j * 64;
+    return (at + 64) * kPer<DT> <= V ? load_whole<DT>(base, at + lane) : load_vec<DT>(base, at + lane, V);
+  }
+  // f(vector, j) for every j, G loads ahead
+  template <int G = 2, class F>
+  EPIC_DEV void vectors(F&& f) const {
+    Vec a[G], b[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if (g < steps) a[g] = load(g);
 #pragma unroll 1
-    for (int j = 0; j < steps; ++j) {
-      const Vec x = load(j);
+    for (int j = 0; j < steps; j += G) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        if (j + G + g < steps) b[g] = load(j + G + g);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        if (j + g < steps) {
+          f(a[g], j + g);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+      for (int g = 0; g < G; ++g) a[g] = b[g];
+    }
+  }
+  template <int G = 2, class F>
+  EPIC_DEV void elements(F&& f) const {
+    vectors<G>([&](const Vec& x, int j) {
 #pragma unroll
       for (int e = 0; e < kPer<DT>; ++e) f(elem<DT>(x, e), id(j) + e);
-    }
+    });
   }
 };
 
-constexpr int kList = 1024;
+constexpr int kList = 256;  // tokens that are put in order in LDS
 
+// BINS: of the histogram.  A step in which a border lies should hold no more
+// than kList tokens: 33 doublings of weight in 1024 steps put 90 of 32768
+// normally distributed logits (deviation 2) in one, so rows of more registers
+// have more.
+template <int BINS>
 struct SampleLds {
-  union {
-    uint64_t hist[kBins];
-    uint64_t sorted[kList];
-  };
-  uint64_t list[kList];  // key of the logit, complement of the id; ascending ids
+  static constexpr int bins = BINS;
+  static constexpr int skew = BINS + BINS / 16;  // 17 words of 8 bytes every 16 bins
+  uint64_t hist[skew];
+  uint64_t list[kList];  // entries, in no order
   uint64_t mass[kMaxWaves];
   float top[kMaxWaves];
-  int count[kMaxWaves];
+  int listed;
   uint64_t before;  // mass (or tokens) above the chosen bin
   uint64_t inside;  // in it
   uint32_t lo, hi;  // keys of the bin
+  uint64_t cut;
   int32_t id;
 };
+EPIC_DEV int slot(int bin) { return bin + (bin >> 4); }
 
-// The wavefront in which the running sum of `mass` exceeds target, and what is
-// left of the target there.
-EPIC_DEV int owner_of(const uint64_t* mass, int waves, uint64_t target, uint64_t& left) {
-  uint64_t before = 0;
-  for (int w = 0; w < waves; ++w) {
-    const uint64_t x = mass[w];
-    if (before + x > target) {
-      left = target - before;
-      return w;
-    }
-    before += x;
-  }
-  left = 0;
-  return -1;
+// The sum of the wavefronts' masses.
+EPIC_DEV uint64_t mass_of(const uint64_t* mass, int waves, int lane) {
+  return wave_sum64(lane < waves ? mass[lane] : 0);
+}
+// The wavefront in which the running sum of `mass` exceeds target (-1: none),
+// and what is left of the target there.
+EPIC_DEV int owner_of(const uint64_t* mass, int waves, int lane, uint64_t target, uint64_t& left) {
+  const uint64_t x = lane < waves ? mass[lane] : 0, upto = scan64(x);
+  const uint64_t over = __ballot(upto > target);
+  if (over == 0) return -1;
+  const int w = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)over) - 1);
+  left = target - lane64(upto - x, w);
+  return w;
 }
 
 // The element of the vectors x of a wavefront (first id of a lane's: `id`) at
@@ -159,21 +191,46 @@ EPIC_DEV void find_element(const Vec& x, int id, uint64_t own, uint64_t left, in
 template <int DT, class P, class F>
 EPIC_DEV void locate(const Row<DT>& row, const uint64_t* mass, int wave, int waves, uint64_t target, P&& part,
                      F&& found) {
-  uint64_t left;
-  if (owner_of(mass, waves, target, left) != wave) return;
-#pragma unroll 1
-  for (int j = 0; j < row.steps; ++j) {
-    const Vec x = row.load(j);
+  uint64_t left = 0;
+  if (owner_of(mass, waves, row.lane, target, left) != wave) return;
+  bool open = true;
+  row.vectors([&](const Vec& x, int j) {
+    if (!open) return;
     uint64_t own = 0;
 #pragma unroll
     for (int e = 0; e < kPer<DT>; ++e) own += part(elem<DT>(x, e), row.id(j) + e);
     const uint64_t all = wave_sum64(own);
     if (all > left) {
+      open = false;
       find_element<DT>(x, row.id(j), own, left, row.lane, part, found);
-      return;
     }
-    left -= all;
+    left -= all;  // not read again once found
+  });
+}
+
+// The bin in which the running sum of the histogram reaches `target` (-1:
+// none), the sum before it and what is in it, by one wavefront.
+template <int BINS>
+EPIC_DEV int scan_bins(const uint64_t* hist, uint64_t target, int lane, uint64_t& before, uint64_t& inside) {
+  constexpr int per = BINS / 64;  // a lane's
+  uint64_t own = 0;
+#pragma unroll 1
+  for (int q = 0; q < per; q += 16) {
+    const uint64_t* at = hist + slot(lane * per + q);
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) own += at[i];
   }
+  const uint64_t upto = scan64(own);
+  const uint64_t reach = __ballot(upto >= target);
+  if (reach == 0) return -1;
+  const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)reach) - 1);
+  const uint64_t base = lane64(upto - own, at);
+  const uint64_t x = lane < per ? hist[slot(at * per + lane)] : 0;
+  const uint64_t sum = base + scan64(x);
+  const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(sum >= target)) - 1);
+  inside = lane64(x, i);
+  before = lane64(sum, i) - inside;
+  return at * per + i;
 }
 
 // The largest key in [lo, hi] for which `holds`, true at lo and, once false,
@@ -192,6 +249,24 @@ EPIC_DEV uint32_t last_key(uint32_t lo, uint32_t hi, int lane, P&& holds) {
   return lo;
 }
 
+// scan_bins by one wavefront for the workgroup.
+template <class LDS>
+EPIC_DEV int border_bin(LDS& s, uint64_t target, int wave, int lane, uint64_t& before) {
+  if (wave == 0) {
+    uint64_t under, inside;
+    const int bin = scan_bins<LDS::bins>(s.hist, target, lane, under, inside);
+    if (lane == 0) {
+      s.id = bin;
+      s.before = under;
+    }
+  }
+  __syncthreads();
+  const int bin = __builtin_amdgcn_readfirstlane(s.id);
+  before = s.before;
+  __syncthreads();
+  return bin;
+}
+
 // Where the ordered tokens' running sum reaches `target`: of their number
 // (MASS false) or their weight (MASS true), counting tokens of the order up to
 // (cut, cut_id) only.  Logits below `least` are not looked at.  Sets (cut,
@@ -202,8 +277,8 @@ EPIC_DEV uint32_t last_key(uint32_t lo, uint32_t hi, int lane, P&& holds) {
 // next round is that bin.  Bins are even steps of the logit; of the key where
 // there are no more keys than bins, and the last round's bin is one key, whose
 // tokens are equal and go by their ids.
-template <int DT, bool MASS>
-EPIC_DEV void find_cut(const Row<DT>& row, SampleLds& s, int wave, int waves, float M, float c, uint64_t target,
+template <int DT, bool MASS, class LDS>
+EPIC_DEV void find_cut(const Row<DT>& row, LDS& s, int wave, int waves, float M, float c, uint64_t target,
                        float least, float& cut, int& cut_id) {
   const int tid = (int)threadIdx.x, threads = waves * 64;
   uint32_t lo = key_of<DT>(least), hi = key_of<DT>(M);
@@ -212,43 +287,32 @@ EPIC_DEV void find_cut(const Row<DT>& row, SampleLds& s, int wave, int waves, fl
   const int old_id = cut_id;
   while (true) {
     const float flo = of_key<DT>(lo), fhi = of_key<DT>(hi);
-    const bool by_key = hi - lo < (uint32_t)kBins;
-    const float scale = (float)kBins * 0.999f / (fhi - flo);
+    const bool by_key = hi - lo < (uint32_t)LDS::bins;
+    const float scale = (float)LDS::bins * 0.999f / (fhi - flo);
     // even steps of the logit need a finite, normal scale
     const bool even = !by_key && scale > 1e-30f && scale < 1e30f;
     int shift = 0;
-    while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
+    while (((hi - lo) >> shift) >= (uint32_t)LDS::bins) ++shift;
     auto bin_of = [&](float l, uint32_t k) {
       const int i = even ? (int)((fhi - l) * scale) : (int)((hi - k) >> shift);
-      return i < 0 ? 0 : i < kBins ? i : kBins - 1;
+      return i < 0 ? 0 : i < LDS::bins ? i : LDS::bins - 1;
     };
-    for (int i = tid; i < kBins; i += threads) s.hist[i] = 0;
+    for (int i = tid; i < LDS::skew; i += threads) s.hist[i] = 0;
     __syncthreads();
     row.elements([&](float l, int id) {
       if (!(l >= flo && l <= fhi)) return;
       if (!(l > old_cut || (l == old_cut && id <= old_id))) return;
       const uint64_t add = MASS ? (uint64_t)weight(l, M, c) : 1ull;
-      atomicAdd((unsigned long long*)&s.hist[bin_of(l, key_of<DT>(l))], (unsigned long long)add);
+      atomicAdd((unsigned long long*)&s.hist[slot(bin_of(l, key_of<DT>(l)))], (unsigned long long)add);
     });
     __syncthreads();
     if (wave == 0) {
-      uint64_t own = 0;
       const int lane = row.lane;
-      for (int i = 0; i < kBins / 64; ++i) own += s.hist[lane * (kBins / 64) + i];
-      const uint64_t upto = scan64(own);
-      const uint64_t reach = __ballot(upto >= target);
-      if (reach == 0) {
+      uint64_t before, inside;
+      const int bin = scan_bins<LDS::bins>(s.hist, target, lane, before, inside);
+      if (bin < 0) {
         if (lane == 0) s.id = -1;
       } else {
-        const int at = __ffsll((unsigned long long)reach) - 1;
-        const uint64_t base = lane64(upto - own, at);
-        uint64_t before = base;
-        int bin = at * (kBins / 64);
-        uint64_t inside = s.hist[bin];
-        while (before + inside < target) {
-          before += inside;
-          inside = s.hist[++bin];
-        }
         // the keys of the bin
         const uint32_t top = last_key(lo, hi, lane, [&](uint32_t k) { return bin_of(of_key<DT>(k), k) >= bin; });
         const bool all = bin_of(flo, lo) <= bin;
@@ -297,140 +361,272 @@ EPIC_DEV void find_cut(const Row<DT>& row, SampleLds& s, int wave, int waves, fl
   }
 }
 
-EPIC_DEV uint64_t swap64(uint64_t v, int x) {
-  return ((uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), x, 64) << 32) | (uint32_t)__shfl_xor((int)v, x, 64);
+// lane i's value in lane i ^ X
+template <int X>
+EPIC_DEV uint32_t swap32(uint32_t v) {
+  if constexpr (X == 1) return dpp<0xB1>(0u, v);
+  if constexpr (X == 2) return dpp<0x4E>(0u, v);
+  if constexpr (X == 4) return dpp<0x1B>(0u, dpp<0x141>(0u, v));  // ^7, then ^3
+  if constexpr (X == 8) return dpp<0x128>(0u, v);                 // rotate the row of 16 by 8
+  if constexpr (X == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return __builtin_amdgcn_inverse_ballot_w64(0xFFFF0000FFFF0000ull) ? r[0] : r[1];
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_amdgcn_inverse_ballot_w64(0xFFFFFFFF00000000ull) ? r[0] : r[1];
 }
-// lanes x apart in order: the larger key in the lane with `up`
-EPIC_DEV uint64_t order64(uint64_t v, int x, bool up) {
-  const uint64_t o = swap64(v, x);
-  return (v > o) == up ? v : o;
+// lanes X apart in order: the larger key in the lanes of `up`
+template <int X>
+EPIC_DEV uint64_t order64(uint64_t v, uint64_t up) {
+  const uint64_t o = ((uint64_t)swap32<X>((uint32_t)(v >> 32)) << 32) | swap32<X>((uint32_t)v);
+  return (v > o) == __builtin_amdgcn_inverse_ballot_w64(up) ? v : o;
 }
-// 64 keys, descending by lane
-EPIC_DEV uint64_t sort64(uint64_t v, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-    for (int x = k >> 1; x > 0; x >>= 1) v = order64(v, x, ((lane & k) == 0) == ((lane & x) == 0));
+constexpr uint64_t lanes_without(int bit) {
+  uint64_t m = 0;
+  for (int i = 0; i < 64; ++i) m |= (uint64_t)((i & bit) == 0) << i;
+  return m;
+}
+template <int K, int X>
+EPIC_DEV uint64_t sort_step(uint64_t v) {
+  constexpr uint64_t up = ~(lanes_without(K) ^ lanes_without(X));
+  v = order64<X>(v, up);
+  if constexpr (X > 1) return sort_step<K, X / 2>(v);
   return v;
 }
-// The token drawn from a list of N tokens in the order of their ids, in which
-// all that the filters can keep are found.  k: top-k or INT32_MAX; P: top-p in
-// 2^24ths; S: the mass that P is a share of, or 0 for the mass of the first k.
-// Called by the whole workgroup, `found` by one lane of it.
-template <int DT, class F>
-EPIC_DEV void draw_from_list(SampleLds& s, int N, int wave, int waves, float M, float c, int k, uint32_t P, uint64_t S,
-                             uint32_t least, uint32_t U, F&& found) {
-  const int tid = (int)threadIdx.x, lane = tid & 63;
-  auto weigh = [&](uint64_t key) { return key ? (uint64_t)weight(of_key<DT>((uint32_t)(key >> 32)), M, c) : 0ull; };
-  if (N <= 64) {  // one wavefront, a token a lane
-    if (wave != 0) return;
-    const uint64_t mine = lane < N ? s.list[lane] : 0;
-    const uint64_t ranked = sort64(mine, lane);
-    const uint64_t w = lane < k ? weigh(ranked) : 0;
-    const uint64_t upto = scan64(w);
-    if (S == 0) S = lane64(upto, 63);
-    const uint64_t want = share(S, P), need = want > 0 ? want : 1;
-    // the tokens whose mass before is short of the need: a prefix of the order
-    const uint64_t prefix = __ballot(lane < N && lane < k && upto - w < need);
-    const uint64_t last = lane64(ranked, 63 - __clzll((long long)(prefix | 1)));
-    uint64_t kept = weigh(mine);
-    if (mine < last || kept < least) kept = 0;
-    const uint64_t sum = scan64(kept);
-    const uint64_t target = share(lane64(sum, 63), U);
-    const uint64_t here = __ballot(sum > target);
-    if (lane == __ffsll((unsigned long long)here) - 1)
-      found((int)~(uint32_t)mine, of_key<DT>((uint32_t)(mine >> 32)));
-    return;
-  }
-  int size = 128;
-  while (size < N) size *= 2;
-  const int threads = waves * 64;
-  for (int i = tid; i < size; i += threads) s.sorted[i] = i < N ? s.list[i] : 0;
-  for (int run = 2; run <= size; run *= 2)
-    for (int x = run / 2; x > 0; x /= 2) {
-      __syncthreads();
-      for (int p = tid; p < size / 2; p += threads) {
-        const int i = 2 * p - (p & (x - 1)), j = i + x;
-        const uint64_t a = s.sorted[i], b = s.sorted[j];
-        if ((a < b) == ((i & run) == 0)) {
-          s.sorted[i] = b;
-          s.sorted[j] = a;
-        }
-      }
-    }
-  __syncthreads();
-  if (wave != 0) return;
-  const int per = size / 64;  // a lane's tokens, adjacent
-  uint64_t own = 0;
-  for (int i = lane * per; i < lane * per + per; ++i)
-    if (i < k) own += weigh(s.sorted[i]);
-  uint64_t upto = scan64(own);
-  if (S == 0) S = lane64(upto, 63);
-  const uint64_t want = share(S, P), need = want > 0 ? want : 1;
-  uint64_t before = upto - own, mine = ~0ull;  // the lane's last token of the prefix
-  for (int i = lane * per; i < lane * per + per; ++i) {
-    if (i >= N || i >= k || before >= need) break;
-    mine = s.sorted[i];
-    before += weigh(mine);
-  }
-  const uint64_t some = __ballot(mine != ~0ull);
-  const uint64_t last = lane64(mine, 63 - __clzll((long long)(some | 1)));
-  auto kept = [&](int i) -> uint64_t {
-    const uint64_t key = i < N ? s.list[i] : 0, w = weigh(key);
-    return key < last || w < least ? 0 : w;
-  };
-  own = 0;
-  for (int i = lane * per; i < lane * per + per; ++i) own += kept(i);
-  upto = scan64(own);
-  const uint64_t target = share(lane64(upto, 63), U);
-  const uint64_t here = __ballot(upto > target);
-  if (lane != __ffsll((unsigned long long)here) - 1) return;
-  uint64_t rest = target - (upto - own);
-  for (int i = lane * per; i < lane * per + per; ++i) {
-    const uint64_t w = kept(i);
-    if (w > rest) {
-      found((int)~(uint32_t)s.list[i], of_key<DT>((uint32_t)(s.list[i] >> 32)));
-      return;
-    }
-    rest -= w;
-  }
+// 64 keys, descending by lane (bitonic)
+EPIC_DEV uint64_t sort64(uint64_t v) {
+  v = sort_step<2, 1>(v);
+  v = sort_step<4, 2>(v);
+  v = sort_step<8, 4>(v);
+  v = sort_step<16, 8>(v);
+  v = sort_step<32, 16>(v);
+  return sort_step<64, 32>(v);
 }
 
-// A logit that at least k of the workgroup's lanes' largest reach, hence at
-// least k logits: a lower bound of the k-th largest.  `none` when fewer than k
-// lanes have one of any weight.
-template <int DT>
-EPIC_DEV float bound_of_top(SampleLds& s, float mine, int wave, int waves, float M, float c, int k, float none) {
+// A token of a list: greater means earlier in the order.
+EPIC_DEV uint64_t entry(uint32_t key, int id) { return ((uint64_t)key << 32) | (uint32_t)~id; }
+EPIC_DEV uint32_t key_in(uint64_t e) { return (uint32_t)(e >> 32); }
+EPIC_DEV int id_in(uint64_t e) { return (int)~(uint32_t)e; }
+
+// the highest bit of an id
+EPIC_DEV int top_bit(int V) { return V > 1 ? 1 << (31 - __clz(V - 1)) : 0; }
+
+// Sum over a wavefront: of numbers of entries by ballots, of weights by lanes.
+template <bool MASS, int R, class P>
+EPIC_DEV uint64_t sum_where(const uint32_t (&w)[R], P&& is) {
+  uint64_t sum = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if constexpr (MASS)
+      sum += is(r) ? w[r] : 0u;
+    else
+      sum += (uint64_t)__popcll((unsigned long long)__ballot(is(r)));
+  }
+  return MASS ? wave_sum64(sum) : sum;
+}
+
+// The entry at which the running sum of the weights, in the order of the
+// entries, reaches `target` >= 1 (MASS false: their number does), by one
+// wavefront that holds R entries a lane (0: none, of weight 0).  0 when the
+// sum does not reach it.  A search for the key bit by bit, then for the id
+// among equal keys, whose weights are equal too.
+template <int DT, bool MASS, int R>
+EPIC_DEV uint64_t reach_entry(const uint64_t (&e)[R], const uint32_t (&w)[R], uint64_t target, int V) {
+  uint32_t key = 0;
+#pragma unroll 1
+  for (uint32_t bit = DT == EPIC_F32 ? 0x80000000u : 0x8000u; bit; bit >>= 1) {
+    const uint32_t at = key | bit;
+    if (sum_where<MASS>(w, [&](int r) { return key_in(e[r]) >= at; }) >= target) key = at;
+  }
+  const uint64_t above = sum_where<MASS>(w, [&](int r) { return key_in(e[r]) > key; });
+  const uint64_t equal = sum_where<MASS>(w, [&](int r) { return e[r] != 0 && key_in(e[r]) == key; });
+  if (above + equal < target) return 0;
+  if (above + equal == target) return entry(key, INT32_MAX);
+  int id = 0;
+#pragma unroll 1
+  for (int bit = top_bit(V); bit; bit >>= 1) {
+    const int at = id + bit;
+    if (above + sum_where<MASS>(w, [&](int r) { return key_in(e[r]) == key && id_in(e[r]) < at; }) < target) id = at;
+  }
+  return entry(key, id);
+}
+
+struct Draw {
+  float M, c;
+  int k;           // top-k, INT32_MAX: off
+  uint32_t P;      // top-p in 2^24ths of the mass of the first k
+  uint32_t least;  // min-p
+  uint32_t U;
+  int V;
+};
+
+// The token drawn from a list of N tokens, in which all that the filters can
+// keep are found; by one wavefront, R tokens a lane.
+template <int DT, int R, class F>
+EPIC_DEV void draw_from_list(const uint64_t* list, int N, int lane, const Draw& d, F&& found) {
+  uint64_t e[R];
+  uint32_t w[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    e[r] = r * 64 + lane < N ? list[r * 64 + lane] : 0;
+    w[r] = e[r] ? weight(of_key<DT>(key_in(e[r])), d.M, d.c) : 0;
+  }
+  uint64_t cut = 0;
+  if constexpr (R == 1) {  // in order, a token a lane
+    if (d.k < N || d.P < 16777216u) {
+      const uint64_t ranked = sort64(e[0]);
+      const uint64_t rw = ranked && lane < d.k ? (uint64_t)weight(of_key<DT>(key_in(ranked)), d.M, d.c) : 0;
+      const uint64_t upto = scan64(rw);
+      const uint64_t want = share(lane64(upto, 63), d.P), need = want > 0 ? want : 1;
+      // the tokens whose mass before is short of the need: a prefix of the order
+      const uint64_t prefix = __ballot(ranked != 0 && lane < d.k && upto - rw < need);
+      cut = lane64(ranked, 63 - __clzll((long long)(prefix | 1)));
+    }
+  } else {
+    if (d.k < N) {
+      cut = reach_entry<DT, false>(e, w, (uint64_t)d.k, d.V);
+    }
+    if (d.P < 16777216u) {
+      uint32_t in[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) in[r] = e[r] >= cut ? w[r] : 0;
+      const uint64_t sum = sum_where<true>(in, [&](int) { return true; });
+      const uint64_t want = share(sum, d.P), need = want > 0 ? want : 1;
+      if (need < sum) cut = reach_entry<DT, true>(e, in, need, d.V);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (e[r] < cut || w[r] < d.least) w[r] = 0;
+  int id;
+  if constexpr (R == 1) {  // in the order of the ids, the weights with them
+    const uint64_t by_id = sort64(w[0] ? ((uint64_t)(uint32_t)e[0] << 32) | w[0] : 0);
+    const uint64_t upto = scan64((uint32_t)by_id);
+    const uint64_t here = __ballot(upto > share(lane64(upto, 63), d.U));
+    id = ~__builtin_amdgcn_readlane((int)(by_id >> 32), __ffsll((unsigned long long)here) - 1);
+  } else {  // the last id below which the mass is not over the target
+    const uint64_t target = share(sum_where<true>(w, [&](int) { return true; }), d.U);
+    id = 0;
+#pragma unroll 1
+    for (int bit = top_bit(d.V); bit; bit >>= 1) {
+      const int at = id + bit;
+      if (sum_where<true>(w, [&](int r) { return id_in(e[r]) < at; }) <= target) id = at;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (w[r] && id_in(e[r]) == id) found(id, of_key<DT>(key_in(e[r])));
+}
+
+// A logit that at least k of the lanes' largest of their even and odd vectors
+// reach, hence at least k logits: a lower bound of the k-th largest.  `none`
+// when fewer than k of these have any weight.
+template <class LDS>
+EPIC_DEV float bound_of_top(LDS& s, float mine, float mine2, int wave, int waves, float M, float c, int k, float none) {
   const int tid = (int)threadIdx.x, lane = tid & 63;
-  constexpr int bins = 512;
-  const float scale = c * (bins / 33.0f);
-  for (int i = tid; i < bins; i += waves * 64) s.hist[i] = 0;
+  const float scale = c * (LDS::bins / 33.0f);
+  for (int i = tid; i < LDS::skew; i += waves * 64) s.hist[i] = 0;
   __syncthreads();
-  const float at = (M - mine) * scale;  // M is finite; a lane of nothing but -inf is out
-  if (at < (float)bins) atomicAdd((unsigned long long*)&s.hist[(int)at], 1ull);
+  const float at = (M - mine) * scale, at2 = (M - mine2) * scale;  // M is finite; a lane of nothing but -inf is out
+  if (at < (float)LDS::bins) atomicAdd((unsigned long long*)&s.hist[slot((int)at)], 1ull);
+  if (at2 < (float)LDS::bins) atomicAdd((unsigned long long*)&s.hist[slot((int)at2)], 1ull);
   __syncthreads();
-  uint64_t own = 0;
-  for (int i = 0; i < bins / 64; ++i) own += s.hist[lane * (bins / 64) + i];
-  const uint64_t upto = scan64(own);
-  const uint64_t reach = __ballot(upto >= (uint64_t)k);
-  float bound = none;
-  if (reach) {
-    const int l = __ffsll((unsigned long long)reach) - 1;
-    uint64_t before = lane64(upto - own, l);
-    int bin = l * (bins / 64);
-    while ((before += s.hist[bin]) < (uint64_t)k) ++bin;
-    // the lanes counted have (M - l) * scale < bin + 1; a little below that is below them all
-    const float low = M - (float)(bin + 1) / scale;
-    bound = low - fabsf(low) * 1e-6f - fabsf(M) * 1e-6f;
+  uint64_t before;
+  const int bin = border_bin(s, (uint64_t)k, wave, lane, before);
+  if (bin < 0) return none;
+  // the lanes counted have (M - l) * scale < bin + 1; a little below that is below them all
+  const float low = M - (float)(bin + 1) / scale;
+  return fmaxf(low - fabsf(low) * 1e-6f - fabsf(M) * 1e-6f, none);
+}
+
+template <int DT, class LDS>
+EPIC_DEV void list_token(LDS& s, float l, int id) {
+  const int i = atomicAdd(&s.listed, 1);
+  if (i < kList) s.list[i] = entry(key_of<DT>(l), id);
+}
+
+// The entry among the `count` <= kList tokens of s.list at which the
+// running sum of their numbers or weights reaches target >= 1; by the whole
+// workgroup, of which one wavefront works.
+template <int DT, bool MASS, class LDS>
+EPIC_DEV uint64_t border_entry(LDS& s, int count, uint64_t target, int wave, int lane, int V, float M, float c) {
+  if (wave == 0) {
+    auto weigh = [&](uint64_t e) -> uint32_t {
+      return e == 0 ? 0u : MASS ? weight(of_key<DT>(key_in(e)), M, c) : 1u;
+    };
+    uint64_t cut;
+    if (count <= 64) {
+      const uint64_t ranked = sort64(lane < count ? s.list[lane] : 0);
+      const uint64_t reach = __ballot(scan64(weigh(ranked)) >= target);
+      cut = lane64(ranked, __ffsll((unsigned long long)reach) - 1);
+    } else {
+      constexpr int R = kList / 64;
+      uint64_t e[R];
+      uint32_t w[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        e[r] = r * 64 + lane < count ? s.list[r * 64 + lane] : 0;
+        w[r] = weigh(e[r]);
+      }
+      cut = reach_entry<DT, MASS>(e, w, target, V);
+    }
+    if (lane == 0) s.cut = cut;
   }
   __syncthreads();
-  return fmaxf(bound, none);
+  const uint64_t cut = s.cut;
+  __syncthreads();
+  return cut;
+}
+
+// Where the order's running sum of numbers or weights reaches `target`, as an
+// entry (0: nowhere).  Counts tokens of the order up to `old` only; logits
+// below `low` are not looked at.  One pass for a histogram over even steps of
+// the logit, one to collect the tokens of the step in which the target is
+// reached, which a wavefront puts in order.
+template <int DT, bool MASS, class LDS>
+EPIC_DEV uint64_t border_of(const Row<DT>& row, LDS& s, int wave, int waves, float M, float c, uint64_t target,
+                            float low, uint64_t old) {
+  const int tid = (int)threadIdx.x, lane = row.lane;
+  const float old_l = old ? of_key<DT>(key_in(old)) : -kInf;
+  const int old_id = old ? id_in(old) : INT32_MAX;
+  auto counts = [&](float l, int id) { return l >= low && (l > old_l || (l == old_l && id <= old_id)); };
+  const float scale = (float)(LDS::bins - 1) / (M - low);
+  if (scale > 1e-30f && scale < 1e30f) {
+    for (int i = tid; i < LDS::skew; i += waves * 64) s.hist[i] = 0;
+    if (tid == 0) s.listed = 0;
+    __syncthreads();
+    row.elements([&](float l, int id) {
+      if (counts(l, id)) {
+        const int bin = min((int)((M - l) * scale), LDS::bins - 1);
+        atomicAdd((unsigned long long*)&s.hist[slot(bin)], MASS ? (unsigned long long)weight(l, M, c) : 1ull);
+      }
+    });
+    __syncthreads();
+    uint64_t before;
+    const int bin = border_bin(s, target, wave, lane, before);
+    if (bin < 0) return 0;
+    row.elements([&](float l, int id) {
+      if (counts(l, id) && min((int)((M - l) * scale), LDS::bins - 1) == bin) {
+        list_token<DT>(s, l, id);
+      }
+    });
+    __syncthreads();
+    const int count = s.listed;
+    __syncthreads();
+    if (count <= kList) return border_entry<DT, MASS>(s, count, target - before, wave, lane, row.V, M, c);
+  }
+  float cut_l = old_l;
+  int cut_id = old_id;
+  find_cut<DT, MASS>(row, s, wave, waves, M, c, target, low, cut_l, cut_id);
+  return cut_l == -kInf ? 0 : entry(key_of<DT>(cut_l), cut_id);
 }
 
 template <int DT, int J>
 __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
-  __shared__ SampleLds s;
+  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024>;
+  __shared__ LDS s;
   constexpr int E = kPer<DT>;
+  constexpr float kSteps = -(float)(LDS::bins / 33);  // steps of a doubling
   const int r = (int)blockIdx.x, b = r / a.rows, i = r - b * a.rows;
   const int threads = (int)blockDim.x, waves = threads >> 6;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -449,11 +645,17 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
   row.lane = (int)threadIdx.x & 63;
   row.steps = J ? J : ((a.V + E - 1) / E + threads - 1) / threads;
   row.first = wave * row.steps * 64;
+  asm("" : "+s"(row.steps));  // not a constant: loops over it stay loops
   const int lane = row.lane;
   Vec v[J ? J : 1];
   if constexpr (J > 0) {
+    if ((row.first + J * 64) * E <= a.V) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) v[j] = row.load(j);
+      for (int j = 0; j < J; ++j) v[j] = load_whole<DT>(row.base, row.first + j * 64 + lane);
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) v[j] = row.load(j);
+    }
   }
   // Without this the compiler keeps what one pass computed of every element
   // for the next, which takes more registers than there are.
@@ -473,21 +675,25 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
         __builtin_amdgcn_sched_barrier(0);  // a vector's temporaries at a time
       }
     } else {
-#pragma unroll 1
-      for (int j = 0; j < row.steps; ++j) f(row.load(j), j);
+      row.template vectors<8>(f);
     }
   };
 
-  float mine = -kInf;
-  each([&](const Vec& x, int) {
+  float mine = -kInf, mine2 = -kInf;  // of the lane's even and odd vectors
+  each([&](const Vec& x, int j) {
+    float m = -kInf;
 #pragma unroll
-    for (int e = 0; e < E; ++e) mine = fmaxf(mine, elem<DT>(x, e));
+    for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
+    if (j & 1)
+      mine2 = fmaxf(mine2, m);
+    else
+      mine = fmaxf(mine, m);
   });
-  float M = wave_max(mine);
+  float M = wave_max(fmaxf(mine, mine2));
   if (lane == 0) s.top[wave] = M;
   __syncthreads();
-  for (int w = 0; w < waves; ++w) M = fmaxf(M, s.top[w]);
-  M = lane32(M, 0);
+  const float M_wave = M;
+  M = wave_max(lane < waves ? s.top[lane] : -kInf);
   if (!(M > -kInf && M < kInf)) {  // no finite logit, or one of +inf
     if (threadIdx.x == 0) {
       a.tok[r] = -1;
@@ -509,22 +715,44 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
   const bool by_k = k != INT32_MAX, by_p = P < 16777216u;
 
   forget();
-  uint64_t sums[J ? J : 1] = {};  // the lane's, by vector
-  each([&](const Vec& x, int j) {
-    uint64_t w = 0;
+  uint64_t sums[J > 1 ? J / 2 : 1] = {};  // the lane's, by pair of vectors
+  uint64_t own_of_p = 0;
+  const bool steps_of_p = by_p && !by_k;
+  if (!steps_of_p) {
+    each([&](const Vec& x, int j) {
+      uint64_t w = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) w += weight(elem<DT>(x, e), M, c);
-    sums[J ? j : 0] += w;
-  });
-  uint64_t own = 0;
+      for (int e = 0; e < E; ++e) w += weight(elem<DT>(x, e), M, c);
+      sums[J ? j / 2 : 0] += w;
+    });
+  } else {
+    // With it the weights by steps of the exponent, for top-p's border.  What
+    // top-p leaves out weighs (1 - p) W at least, and W is 2^31 at least: steps
+    // of which no token weighs the V-th part of that are not needed to get there.
+    for (int i = (int)threadIdx.x; i < LDS::skew; i += threads) s.hist[i] = 0;
+    if (threadIdx.x == 0) s.listed = 0;
+    __syncthreads();
+    const float light = (float)(16777216u - P) * (1.f / 16777216.f) / (float)a.V;
+    const float last = fminf(floorf(log2f(light) * kSteps) + 2.f, (float)LDS::bins);
+    row.template vectors<4>([&](const Vec& v, int) {
+      uint64_t all = 0;
 #pragma unroll
-  for (int j = 0; j < (J ? J : 1); ++j) own += sums[j];
+      for (int e = 0; e < E; ++e) {
+        const float x = exponent(elem<DT>(v, e), M, c), step = x * kSteps;
+        const uint32_t w = weight_of(x);
+        all += w;
+        if (step < last) atomicAdd((unsigned long long*)&s.hist[slot((int)step)], (unsigned long long)w);
+      }
+      own_of_p += all;
+    });
+  }
+  uint64_t own = own_of_p;
+#pragma unroll
+  for (int j = 0; j < (J > 1 ? J / 2 : 1); ++j) own += sums[j];
   own = wave_sum64(own);
   if (lane == 0) s.mass[wave] = own;
   __syncthreads();
-  uint64_t W = 0;
-  for (int w = 0; w < waves; ++w) W += s.mass[w];
-  W = lane64(W, 0);
+  const uint64_t W = mass_of(s.mass, waves, lane);
   auto found = [&](int id, float l) {
     a.tok[r] = id;
     a.conf[r] = power(l, M, c) * (kOne / (float)W);
@@ -534,115 +762,153 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
     auto part = [&](float l, int) { return (uint64_t)weight(l, M, c); };
     const uint64_t target = share(W, U);
     if constexpr (J > 0) {
-      uint64_t left;
-      if (owner_of(s.mass, waves, target, left) != wave) return;
-      uint64_t at = 0, mass = 0;
-      Vec x = v[0];
+      uint64_t left = 0;
+      if (owner_of(s.mass, waves, lane, target, left) != wave) return;
       int j = -1;
 #pragma unroll
-      for (int t = 0; t < J; ++t) {
+      for (int t = 0; t < J / 2; ++t) {
         const uint64_t all = wave_sum64(sums[t]);
-        if (j < 0 && all > left) {
-          j = t;
-          x = v[t];
-          mass = sums[t];
-          at = left;
+        if (j < 0) {
+          if (all > left)
+            j = 2 * t;
+          else
+            left -= all;
         }
-        left -= all;  // not read again once found
       }
-      find_element<DT>(x, row.id(j), mass, at, lane, part, found);
+      j = __builtin_amdgcn_readfirstlane(j);
+      Vec x = row.load(j);
+      const Vec y = row.load(j + 1);
+      uint64_t own_x = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) own_x += part(elem<DT>(x, e), 0);
+      const uint64_t all = wave_sum64(own_x);
+      if (all <= left) {
+        left -= all;
+        ++j;
+        x = y;
+        own_x = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) own_x += part(elem<DT>(x, e), 0);
+      }
+      find_element<DT>(x, row.id(j), own_x, left, lane, part, found);
     } else {
       locate(row, s.mass, wave, waves, target, part, found);
     }
     return;
   }
 
-  float cut = -kInf;  // kept: logits above it, and equal ones up to cut_id
-  int cut_id = INT32_MAX;
-  {
-    // tokens further than 33 doublings below the largest weigh nothing; -inf is no token
-    const float far = M - 33.0f / c;
-    const float light = fmaxf(far - fabsf(far) * 1e-5f, kLowest<DT>);
-    float low = light;
-    if (k == 1) {
-      low = M;
-    } else if (by_k) {
-      if (k <= threads) low = bound_of_top<DT>(s, mine, wave, waves, M, c, k, light);
-    } else {
-      // what top-p leaves out, or what min-p does
-      const float part = !by_p ? (float)least : (float)(16777216u - P) * (1.f / 16777216.f) * (float)W / (float)a.V;
-      const float deep = M + (log2f(part * (1.f / kOne)) - 0.01f) / c;
-      low = fmaxf(light, deep - fabsf(deep) * 1e-5f - fabsf(M) * 1e-5f);
-    }
-    low = fminf(low, M);  // rows of the type's lowest values
-    forget();
-    int n = 0;
-    each([&](const Vec& x, int) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) n += elem<DT>(x, e) >= low ? 1 : 0;
+  // tokens further than 33 doublings below the largest weigh nothing; -inf is no token
+  const float far = M - 33.0f / c;
+  const float light = fmaxf(far - fabsf(far) * 1e-5f, kLowest<DT>);
+  auto above = [&](float weighs) {  // a logit below all that weigh as much
+    const float deep = M + (log2f(weighs * (1.f / kOne)) - 0.01f) / c;
+    return fmaxf(light, deep - fabsf(deep) * 1e-5f - fabsf(M) * 1e-5f);
+  };
+  uint64_t cut = 0;  // kept: entries not after it
+  bool summed = false;
+  if (steps_of_p) {
+    const uint64_t want = share(W, P), need = want > 0 ? want : 1;
+    uint64_t before;
+    const int bin = border_bin(s, need, wave, lane, before);
+    // one pass collects the tokens of the border's step and sums those before it
+    const float first = (float)bin;
+    uint64_t some = 0;
+    row.template elements<4>([&](float l, int id) {
+      const float x = exponent(l, M, c), step = x * kSteps;
+      if (step < first) {
+        const uint32_t w = weight_of(x);
+        some += w >= least ? w : 0u;
+      } else if (step < first + 1.f) {
+        list_token<DT>(s, l, id);
+      }
     });
-    n = (int)wave_sum64((uint64_t)n);
-    if (lane == 0) s.count[wave] = n;
+    some = wave_sum64(some);
     __syncthreads();
-    int N = 0, at = 0;
-    for (int w = 0; w < waves; ++w) {
-      if (w == wave) at = N;
-      N += s.count[w];
+    if (lane == 0) s.mass[wave] = some;
+    const int count = s.listed;
+    __syncthreads();
+    if (count <= kList) {
+      cut = border_entry<DT, true>(s, count, need - before, wave, lane, a.V, M, c);
+      // the border's own, to the wavefront that has their ids
+      for (int i = (int)threadIdx.x; i < count; i += threads) {
+        const uint64_t e = s.list[i];
+        const uint32_t w = weight(of_key<DT>(key_in(e)), M, c);
+        if (e >= cut && w >= least)
+          atomicAdd((unsigned long long*)&s.mass[id_in(e) / (row.steps * 64 * E)], (unsigned long long)w);
+      }
+      __syncthreads();
+      summed = true;
+    } else {
+      cut = border_of<DT, true>(row, s, wave, waves, M, c, need, fminf(light, M), 0);
     }
-    N = __builtin_amdgcn_readfirstlane(N);
-    if (N <= kList) {
-      forget();
-      each([&](const Vec& x, int j) {
-        uint32_t in = 0;
+  } else {
+    float low = light;
+    if (k == 1)
+      low = M;
+    else if (by_k && k <= 2 * threads)
+      low = bound_of_top(s, mine, mine2, wave, waves, M, c, k, light);
+    else if (!by_k)
+      low = above((float)least);
+    low = fminf(low, M);  // rows of the type's lowest values
+    if (!by_k || k <= 2 * threads) {
+      if (threadIdx.x == 0) s.listed = 0;
+      __syncthreads();
+      if (M_wave >= low) row.vectors([&](const Vec& x, int j) {
+        float m = -kInf;
 #pragma unroll
-        for (int e = 0; e < E; ++e) in |= elem<DT>(x, e) >= low ? 1u << e : 0u;
-        if (__ballot(in != 0) == 0) return;
-        const int upto = (int)scan64((uint64_t)__popc(in));
-        int to = at + upto - __popc(in);
-        at += __builtin_amdgcn_readlane(upto, 63);
-        for (; in; in &= in - 1) {
-          const int e = __ffs((int)in) - 1;
-          s.list[to++] = ((uint64_t)key_of<DT>(elem_at<DT>(x, e)) << 32) | (uint32_t)~(row.id(j) + e);
-        }
+        for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
+        if (m < low || __hip_atomic_load(&s.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kList) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (elem<DT>(x, e) >= low) list_token<DT>(s, elem<DT>(x, e), row.id(j) + e);
       });
       __syncthreads();
-      draw_from_list<DT>(s, N, wave, waves, M, c, k, P, by_k ? 0 : W, least, U, found);
-      return;
+      const int N = __builtin_amdgcn_readfirstlane(s.listed);
+      if (N <= kList) {
+        if (wave != 0) return;
+        const Draw draw{M, c, k, P, least, U, a.V};
+        if (N <= 64)
+          draw_from_list<DT, 1>(s.list, N, lane, draw, found);
+        else
+          draw_from_list<DT, kList / 64>(s.list, N, lane, draw, found);
+        return;
+      }
+      __syncthreads();
     }
-    // many: by rounds over the row
-    uint64_t S = W;
-    if (by_k) {
-      find_cut<DT, false>(row, s, wave, waves, M, c, (uint64_t)k, low, cut, cut_id);
+    if (by_k) cut = border_of<DT, false>(row, s, wave, waves, M, c, (uint64_t)k, low, 0);
+    if (by_k && by_p) {
+      const float cut_l = cut ? of_key<DT>(key_in(cut)) : -kInf;
+      const int cut_id = cut ? id_in(cut) : INT32_MAX;
       uint64_t some = 0;
       row.elements([&](float l, int id) {
         const uint32_t w = weight(l, M, c);
-        some += (l > cut || (l == cut && id <= cut_id)) ? w : 0u;
+        some += (l > cut_l || (l == cut_l && id <= cut_id)) ? w : 0u;
       });
       some = wave_sum64(some);
       __syncthreads();
       if (lane == 0) s.mass[wave] = some;
       __syncthreads();
-      S = 0;
-      for (int w = 0; w < waves; ++w) S += s.mass[w];
-    }
-    if (by_p) {
+      const uint64_t S = mass_of(s.mass, waves, lane);
       const uint64_t want = share(S, P);
       __syncthreads();
-      find_cut<DT, true>(row, s, wave, waves, M, c, want > 0 ? want : 1, low, cut, cut_id);
+      cut = border_of<DT, true>(row, s, wave, waves, M, c, want > 0 ? want : 1, low, cut);
     }
   }
+  const float cut_l = cut ? of_key<DT>(key_in(cut)) : -kInf;
+  const int cut_id = cut ? id_in(cut) : INT32_MAX;
   auto kept = [&](float l, int id) -> uint64_t {
     const uint32_t w = weight(l, M, c);
-    return (l > cut || (l == cut && id <= cut_id)) && w >= least ? w : 0u;
+    return (l > cut_l || (l == cut_l && id <= cut_id)) && w >= least ? w : 0u;
   };
-  uint64_t some = 0;
-  row.elements([&](float l, int id) { some += kept(l, id); });
-  some = wave_sum64(some);
-  __syncthreads();
-  if (lane == 0) s.mass[wave] = some;
-  __syncthreads();
-  uint64_t D = 0;
-  for (int w = 0; w < waves; ++w) D += s.mass[w];
+  if (!summed) {  // the wavefronts' sums are still to be made
+    uint64_t some = 0;
+    row.elements([&](float l, int id) { some += kept(l, id); });
+    some = wave_sum64(some);
+    __syncthreads();
+    if (lane == 0) s.mass[wave] = some;
+    __syncthreads();
+  }
+  const uint64_t D = mass_of(s.mass, waves, lane);
   locate(row, s.mass, wave, waves, share(D, U), kept, found);
 }
 
@@ -675,13 +941,13 @@ EPIC_DEV uint64_t propose_key(int32_t t, float f, int row) {
   return ((uint64_t)k << 32) | (uint32_t)~row;
 }
 
-// the best 64 of two descending lists, descending
-EPIC_DEV uint64_t merge64(uint64_t a, uint64_t b, int lane) {
-  const uint64_t r = swap64(b, 63);
-  uint64_t v = a > r ? a : r;
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) v = order64(v, x, (lane & x) == 0);
-  return v;
+EPIC_DEV uint64_t reversed(uint64_t v, int lane) {
+  return ((uint64_t)(uint32_t)__shfl((int)(v >> 32), 63 - lane, 64) << 32) | (uint32_t)__shfl((int)v, 63 - lane, 64);
+}
+// the best 64 of two lists, a descending and b ascending, descending
+EPIC_DEV uint64_t merge64(uint64_t a, uint64_t b) {
+  // the greater of the first and the last, and so on, are the best 64, and bitonic
+  return sort_step<64, 32>(a > b ? a : b);
 }
 
 // min(P, rows of sequence b with a token), by one wavefront
@@ -734,8 +1000,8 @@ __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
   uint64_t best = 0;
   for (int at = wave * 64; at < a.m; at += waves * 64) {
     const int i = at + lane;
-    const uint64_t k = sort64(i < a.m ? propose_key(tok[i], conf[i], i) : 0, lane);
-    best = at == wave * 64 ? k : merge64(best, k, lane);
+    const uint64_t k = sort64(i < a.m ? propose_key(tok[i], conf[i], i) : 0);
+    best = at == wave * 64 ? k : merge64(best, reversed(k, lane));
   }
   int off = 0, total = 0;
   if constexpr (!COUNTED) {
@@ -759,7 +1025,7 @@ __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
   for (int half = 1; half < waves; half <<= 1) {
     list[wave][lane] = best;
     __syncthreads();
-    if ((wave & (2 * half - 1)) == 0 && wave + half < waves) best = merge64(best, list[wave + half][lane], lane);
+    if ((wave & (2 * half - 1)) == 0 && wave + half < waves) best = merge64(best, list[wave + half][63 - lane]);
     __syncthreads();
   }
   if (wave != 0) return;
@@ -792,6 +1058,12 @@ epic_status launch_sample(const SampleArgs& a, int blocks, hipStream_t stream) {
   const int nvec = (a.V + kPer<DT> - 1) / kPer<DT>;
   auto threads = [&](int J) { return std::max(64, ((nvec + J - 1) / J + 63) / 64 * 64); };
 #define EPIC_SAMPLE(J, NT) hipLaunchKernelGGL((sample_kernel<DT, J>), dim3(blocks), dim3(NT), 0, stream, a)
+  // Eight vectors a lane up to 512 lanes: three workgroups fit a CU.  Sixteen
+  // from there on (2048 rows of 40960 bfloat16 logits 47 us against 55, of
+  // 65536 62 against 85: wider workgroups of eight fit one a CU); at 32768
+  // sixteen take 33 us against 36 without filters, but 2867 rows of mixed
+  // settings 185 against 115, as fewer lanes give a looser bound for top-k.
+  // Four and two for short rows (512 rows of 4096 with top-p 17 us against 25).
   if (nvec <= 2 * 64)
     EPIC_SAMPLE(2, threads(2));
   else if (nvec <= 4 * 256)

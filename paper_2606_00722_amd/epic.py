@@ -323,6 +323,7 @@ def _dtypes() -> dict:
     if not _DTYPES:
         import torch
 
+        lib()
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _DTYPES.update(i32=torch.int32, f32=torch.float32)
     return _DTYPES
@@ -366,12 +367,15 @@ def _call(fn, device, stream, *args):
     the tensors' device current."""
     import torch
 
-    s = torch.cuda.current_stream(device) if stream is None else stream
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(device.index)  # current_stream() builds an object: 2.6 us against 0.05
+    else:
+        s = stream.cuda_stream
     if torch.cuda.current_device() == device.index:
-        _check(fn, getattr(lib(), fn)(*args, s.cuda_stream))
+        _check(fn, getattr(_lib, fn)(*args, s))
     else:
         with torch.cuda.device(device):
-            _check(fn, getattr(lib(), fn)(*args, s.cuda_stream))
+            _check(fn, getattr(_lib, fn)(*args, s))
 
 
 def sample(logits, seqs, uniform, tok, conf, start=None, temperature=None, top_k=None, top_p=None, min_p=None,
