@@ -12,6 +12,7 @@ struct DistillArgs {
   const int32_t* idx;
   const float* logit;
   int K;
+  int steps;  // vectors a lane
   const float* teacher_lse;
   float tau;
   float* loss;          // forward
@@ -135,13 +136,14 @@ struct DistillLds {
   int dead;
 };
 
-// Forward: one workgroup per row.  The row is read once into registers (J
-// vectors a lane; J = 0: read again by each of the two passes).  Listed tokens
-// are marked in a bitmap in LDS and made -inf, so that what is left is the
-// rest; its largest logit and sum are found in one pass over the registers,
-// the listed ones' by a wavefront.  The gradient is a second pass over the
-// registers: every element as one of the rest (0 where it was listed), then
-// the listed ones.
+// Forward: one workgroup per row, one reading of it.  Listed tokens are marked
+// in a bitmap in LDS and made -inf as the vectors arrive, so that what is left
+// is the rest, of which every lane keeps a running maximum and sum; the listed
+// ones are summed by a wavefront.  With the gradient the row stays in registers
+// (J vectors a lane; J = 0, rows too long for that: read again) and is written
+// as the rest's derivative (0 where it was listed), then the listed ones over
+// it.  The sums and shares are float32 relative to their largest; gradients are
+// rounded once, to the logits' type.
 template <int DT, int J, bool GRAD>
 __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
   extern __shared__ uint32_t dyn[];
@@ -162,12 +164,21 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
   const char* row = a.data + b * a.seq_stride + i * a.row_stride;
   const int words = (a.V + 31) / 32, K = a.K;
   Entries ent{(int32_t*)dyn + words, (float*)dyn + words + K, (float*)dyn + words + 2 * K};
-  const int steps = J ? J : ((a.V + E - 1) / E + threads - 1) / threads;
+  const int steps = J ? J : a.steps;
   const int first = wave * steps * 64 + lane;
   Vec v[J ? J : 1];
+  auto load = [&](int j) {
+    const int at = first - lane + j * 64;  // of the wavefront
+    return (at + 64) * E <= a.V ? load_whole<DT>(row, at + lane) : load_vec<DT>(row, at + lane, a.V);
+  };
   if constexpr (J > 0) {
+    if ((first - lane + J * 64) * E <= a.V) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) v[j] = load_vec<DT>(row, first + j * 64, a.V);
+      for (int j = 0; j < J; ++j) v[j] = load_whole<DT>(row, first + j * 64);
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) v[j] = load(j);
+    }
   }
   for (int w = tid; w < words; w += threads) dyn[w] = 0;
   if (tid == 0) s.bad = s.twice = 0;
@@ -211,46 +222,45 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
     }
     return x;
   };
-  // Without this the compiler keeps what one pass computed of every element
-  // for the next, which takes more registers than there are.
-  auto forget = [&] {
-#pragma unroll
-    for (int j = 0; j < (J ? J : 1); ++j)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(v[j].d[k]));
-  };
+  // A running maximum and sum of the lane, one vector after another as they
+  // arrive.
   float top = -kInf, sum = 0.f;
+  auto add = [&](const Vec& x) {
+    float m = top;
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
+    const float by = m > -kInf ? m : 0.f;
+    float some = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) some += __builtin_amdgcn_exp2f((elem<DT>(x, e) - by) * c);
+    sum = sum * __builtin_amdgcn_exp2f((top - by) * c) + some;
+    top = m;
+  };
   if constexpr (J > 0) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       v[j] = rest(v[j], first + j * 64);
-#pragma unroll
-      for (int e = 0; e < E; ++e) top = fmaxf(top, elem<DT>(v[j], e));
+      add(v[j]);
       __builtin_amdgcn_sched_barrier(0);  // a vector's temporaries at a time
     }
-    top = wave_max(top);
-    const float by = top > -kInf ? top : 0.f;
-    forget();
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f((elem<DT>(v[j], e) - by) * c);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    sum = wave_sum(sum);
   } else {
-    // a running maximum and sum
-    for (int j = 0; j < steps; ++j) {
-      const Vec x = rest(load_vec<DT>(row, first + j * 64, a.V), first + j * 64);
-      float m = top;
+    constexpr int G = 4;  // loads ahead
+    Vec x[G], y[G];
 #pragma unroll
-      for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
-      const float by = m > -kInf ? m : 0.f;
-      sum *= __builtin_amdgcn_exp2f((top - by) * c);
-      top = m;
+    for (int g = 0; g < G; ++g) x[g] = load(g < steps ? g : steps - 1);
+#pragma unroll 1
+    for (int j = 0; j < steps; j += G) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f((elem<DT>(x, e) - by) * c);
+      for (int g = 0; g < G; ++g)
+        if (j + G + g < steps) y[g] = load(j + G + g);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        if (j + g < steps) add(rest(x[g], first + (j + g) * 64));
+#pragma unroll
+      for (int g = 0; g < G; ++g) x[g] = y[g];
     }
+  }
+  {
     const float m = wave_max(top), by = m > -kInf ? m : 0.f;
     sum = wave_sum(sum * __builtin_amdgcn_exp2f((top - by) * c));
     top = m;
@@ -320,14 +330,19 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
       if (at * E < a.V) store_vec<DT>(grow, at, a.V, g);
     };
     if constexpr (J > 0) {
-      forget();
+      // Without this the compiler keeps what the pass before computed of every
+      // element, which takes more registers than there are.
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(v[j].d[k]));
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         write(v[j], first + j * 64);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      for (int j = 0; j < steps; ++j) write(rest(load_vec<DT>(row, first + j * 64, a.V), first + j * 64), first + j * 64);
+      for (int j = 0; j < steps; ++j) write(rest(load(j), first + j * 64), first + j * 64);
     }
     __syncthreads();
     const bool twice = s.twice != 0;
@@ -405,21 +420,30 @@ __global__ void __launch_bounds__(1024) distill_backward_kernel(DistillArgs a) {
 }
 
 template <int DT, bool GRAD>
-void launch_forward(const DistillArgs& a, int blocks, hipStream_t stream) {
+void launch_forward(DistillArgs a, int blocks, hipStream_t stream) {
   const int nvec = (a.V + kPer<DT> - 1) / kPer<DT>;
   const size_t lds = ((size_t)(a.V + 31) / 32 + 3 * (size_t)a.K) * 4;
   auto threads = [&](int J) { return std::max(64, ((nvec + J - 1) / J + 63) / 64 * 64); };
-#define EPIC_DISTILL(J, NT) hipLaunchKernelGGL((distill_forward_kernel<DT, J, GRAD>), dim3(blocks), dim3(NT), lds, stream, a)
-  if (nvec <= 2 * 64)
-    EPIC_DISTILL(2, threads(2));
-  else if (nvec <= 4 * 256)
-    EPIC_DISTILL(4, threads(4));
-  else if (nvec <= 8 * 512)
-    EPIC_DISTILL(8, threads(8));
-  else if (nvec <= 16 * 1024)
-    EPIC_DISTILL(16, threads(16));
-  else
-    EPIC_DISTILL(0, 1024);
+  // As many vectors a lane as keep two workgroups or more on a CU.  2048 rows of
+  // 32768 bfloat16 logits, losses and gradient: eight 68 us, sixteen 71, none in
+  // registers 91; of 65536: sixteen 123 us, eight 126 and none 157.
+  const int J = nvec <= 2 * 64 ? 2 : nvec <= 4 * 256 ? 4 : nvec <= 8 * 512 ? 8 : nvec <= 16 * 1024 ? 16 : 0;
+  const int NT = J ? threads(J) : 1024;
+  // Losses alone keep nothing in registers, but deal the row to the lanes alike,
+  // so that their bits are those of a call with the gradient.
+  a.steps = J ? J : (nvec + NT - 1) / NT;
+#define EPIC_DISTILL(J) hipLaunchKernelGGL((distill_forward_kernel<DT, J, GRAD>), dim3(blocks), dim3(NT), lds, stream, a)
+  if constexpr (!GRAD) {
+    EPIC_DISTILL(0);
+  } else {
+    switch (J) {
+      case 2: EPIC_DISTILL(2); break;
+      case 4: EPIC_DISTILL(4); break;
+      case 8: EPIC_DISTILL(8); break;
+      case 16: EPIC_DISTILL(16); break;
+      default: EPIC_DISTILL(0);
+    }
+  }
 #undef EPIC_DISTILL
 }
 
@@ -456,7 +480,7 @@ epic_status distill(const epic_rows_desc* logits, const int32_t* d_seqs, int32_t
   if (!d_top_idx || !d_top_logit || !d_stats || (forward && !d_loss)) return EPIC_ERR_NULL;
   const int es = elem_size(logits->dtype);
   DistillArgs a{(const char*)logits->data, logits->seq_stride * es, logits->row_stride * es, logits->rows, logits->vocab,
-                {d_seqs, d_start, n}, d_top_idx, d_top_logit, K, d_teacher_lse, tau, d_loss, d_stats, d_weight,
+                {d_seqs, d_start, n}, d_top_idx, d_top_logit, K, 0, d_teacher_lse, tau, d_loss, d_stats, d_weight,
                 grad ? (char*)grad->data : nullptr, grad ? grad->seq_stride * es : 0, grad ? grad->row_stride * es : 0};
   const int blocks = logits->batch * logits->rows;
   switch (logits->dtype) {

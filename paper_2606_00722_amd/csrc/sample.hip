@@ -962,16 +962,44 @@ EPIC_DEV int count_rows(const ProposeArgs& a, int b, int lane) {
   return min(n, a.P);
 }
 
+// Eight sequences' counts at once, first, first + step, ...: most are settled by
+// the first 64 rows, whose loads are all in flight together.
+constexpr int kCounts = 8;
+EPIC_DEV void count_eight(const ProposeArgs& a, int first, int step, int lane, int (&n)[kCounts]) {
+  int32_t t[kCounts];
+  float f[kCounts];
+#pragma unroll
+  for (int g = 0; g < kCounts; ++g) {
+    const int b = first + g * step;
+    t[g] = -1;
+    f[g] = 0.f;
+    if (b < a.B && lane < a.m) {
+      t[g] = a.tok[(int64_t)b * a.m + lane];
+      f[g] = a.conf[(int64_t)b * a.m + lane];
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < kCounts; ++g) {
+    n[g] = min(__popcll((unsigned long long)__ballot(proposes(t[g], f[g]))), a.P);
+    const int b = first + g * step;
+    if (n[g] < a.P && a.m > 64 && b < a.B) n[g] = count_rows(a, b, lane);
+  }
+}
+
 // the offsets of a large batch: one workgroup, sequences dealt to wavefronts
 __global__ void __launch_bounds__(1024) propose_count_kernel(ProposeArgs a) {
   __shared__ int n[1024];
   __shared__ int base;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid == 0) base = a.offsets[0] = 0;
   for (int b0 = 0; b0 < a.B; b0 += 1024) {
-    for (int k = wave; k < 1024; k += 16) {
-      const int c = b0 + k < a.B ? count_rows(a, b0 + k, lane) : 0;
-      if (lane == 0) n[k] = c;
+#pragma unroll 1
+    for (int k = wave * kCounts; k < 1024; k += 16 * kCounts) {
+      int c[kCounts];
+      count_eight(a, b0 + k, 1, lane, c);
+#pragma unroll
+      for (int g = 0; g < kCounts; ++g)
+        if (lane == g) n[k + g] = c[g];
     }
     __syncthreads();
     if (wave == 0) {
@@ -992,7 +1020,7 @@ __global__ void __launch_bounds__(1024) propose_count_kernel(ProposeArgs a) {
 template <bool COUNTED>
 __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
   __shared__ uint64_t list[kMaxWaves][64];
-  __shared__ int part[kMaxWaves];
+  __shared__ int part[kMaxWaves], parts[kMaxWaves];
   const int b = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (int)blockDim.x >> 6;
   const int32_t* tok = a.tok + (int64_t)b * a.m;
@@ -1006,18 +1034,20 @@ __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
   int off = 0, total = 0;
   if constexpr (!COUNTED) {
     int before = 0, all = 0;
-    for (int o = wave; o < a.B; o += waves) {
-      const int c = count_rows(a, o, lane);
-      before += o < b ? c : 0;
-      all += c;
+#pragma unroll 1
+    for (int o = wave; o < a.B; o += waves * kCounts) {
+      int c[kCounts];
+      count_eight(a, o, waves, lane, c);
+#pragma unroll
+      for (int g = 0; g < kCounts; ++g) {
+        before += o + g * waves < b ? c[g] : 0;
+        all += c[g];
+      }
     }
-    if (lane == 0) part[wave] = before;
-    __syncthreads();
-    for (int w = 0; w < waves; ++w) off += part[w];
-    __syncthreads();
-    if (lane == 0) part[wave] = all;
-    __syncthreads();
-    for (int w = 0; w < waves; ++w) total += part[w];
+    if (lane == 0) {
+      part[wave] = before;
+      parts[wave] = all;
+    }
   } else {
     off = a.offsets[b];
     total = a.offsets[a.B];
@@ -1027,6 +1057,11 @@ __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
     __syncthreads();
     if ((wave & (2 * half - 1)) == 0 && wave + half < waves) best = merge64(best, list[wave + half][63 - lane]);
     __syncthreads();
+  }
+  if constexpr (!COUNTED) {
+    if (waves == 1) __syncthreads();
+    off = (int)wave_sum64(lane < waves ? (uint64_t)part[lane] : 0);
+    total = (int)wave_sum64(lane < waves ? (uint64_t)parts[lane] : 0);
   }
   if (wave != 0) return;
   const int mine = __popcll((unsigned long long)__ballot(best != 0 && lane < a.P));
@@ -1112,7 +1147,8 @@ epic_status epic_propose(const int32_t* d_tok, const float* d_conf, int32_t batc
   if (batch > 0 && rows > 0 && (!d_tok || !d_conf)) return EPIC_ERR_NULL;
   ProposeArgs a{d_tok, d_conf, d_start, d_cand_seq, d_cand_pos, d_cand_tok, d_cand_conf, d_offsets, batch, rows, per_seq};
   const int threads = std::min(1024, std::max(64, (rows + 63) / 64 * 64));
-  if (batch > 0 && batch <= 256) {
+  // in one launch while no wavefront has more than 16 sequences to count
+  if (batch > 0 && batch <= 16 * (threads / 64)) {
     hipLaunchKernelGGL(propose_kernel<false>, dim3(batch), dim3(threads), 0, stream, a);
   } else {
     hipLaunchKernelGGL(propose_count_kernel, dim3(1), dim3(1024), 0, stream, a);
