@@ -216,9 +216,9 @@ EPIC_DEV int scan_bins(const uint64_t* hist, uint64_t target, int lane, uint64_t
   uint64_t own = 0;
 #pragma unroll 1
   for (int q = 0; q < per; q += 16) {
-    const uint64_t* at = hist + slot(lane * per + q);
+    const uint64_t* at = hist + slot(lane * per + q);  // 8 or 16 bins between two gaps
 #pragma unroll 4
-    for (int i = 0; i < 16; ++i) own += at[i];
+    for (int i = 0; i < (per < 16 ? per : 16); ++i) own += at[i];
   }
   const uint64_t upto = scan64(own);
   const uint64_t reach = __ballot(upto >= target);
@@ -250,11 +250,11 @@ EPIC_DEV uint32_t last_key(uint32_t lo, uint32_t hi, int lane, P&& holds) {
 }
 
 // scan_bins by one wavefront for the workgroup.
-template <class LDS>
+template <int BINS, class LDS>
 EPIC_DEV int border_bin(LDS& s, uint64_t target, int wave, int lane, uint64_t& before) {
   if (wave == 0) {
     uint64_t under, inside;
-    const int bin = scan_bins<LDS::bins>(s.hist, target, lane, under, inside);
+    const int bin = scan_bins<BINS>(s.hist, target, lane, under, inside);
     if (lane == 0) {
       s.id = bin;
       s.before = under;
@@ -524,15 +524,16 @@ EPIC_DEV void draw_from_list(const uint64_t* list, int N, int lane, const Draw& 
 template <class LDS>
 EPIC_DEV float bound_of_top(LDS& s, float mine, float mine2, int wave, int waves, float M, float c, int k, float none) {
   const int tid = (int)threadIdx.x, lane = tid & 63;
-  const float scale = c * (LDS::bins / 33.0f);
-  for (int i = tid; i < LDS::skew; i += waves * 64) s.hist[i] = 0;
+  constexpr int bins = 512;
+  const float scale = c * (bins / 33.0f);
+  for (int i = tid; i < bins + bins / 16; i += waves * 64) s.hist[i] = 0;
   __syncthreads();
   const float at = (M - mine) * scale, at2 = (M - mine2) * scale;  // M is finite; a lane of nothing but -inf is out
-  if (at < (float)LDS::bins) atomicAdd((unsigned long long*)&s.hist[slot((int)at)], 1ull);
-  if (at2 < (float)LDS::bins) atomicAdd((unsigned long long*)&s.hist[slot((int)at2)], 1ull);
+  if (at < (float)bins) atomicAdd((unsigned long long*)&s.hist[slot((int)at)], 1ull);
+  if (at2 < (float)bins) atomicAdd((unsigned long long*)&s.hist[slot((int)at2)], 1ull);
   __syncthreads();
   uint64_t before;
-  const int bin = border_bin(s, (uint64_t)k, wave, lane, before);
+  const int bin = border_bin<bins>(s, (uint64_t)k, wave, lane, before);
   if (bin < 0) return none;
   // the lanes counted have (M - l) * scale < bin + 1; a little below that is below them all
   const float low = M - (float)(bin + 1) / scale;
@@ -603,7 +604,7 @@ EPIC_DEV uint64_t border_of(const Row<DT>& row, LDS& s, int wave, int waves, flo
     });
     __syncthreads();
     uint64_t before;
-    const int bin = border_bin(s, target, wave, lane, before);
+    const int bin = border_bin<LDS::bins>(s, target, wave, lane, before);
     if (bin < 0) return 0;
     row.elements([&](float l, int id) {
       if (counts(l, id) && min((int)((M - l) * scale), LDS::bins - 1) == bin) {
@@ -809,7 +810,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
   if (steps_of_p) {
     const uint64_t want = share(W, P), need = want > 0 ? want : 1;
     uint64_t before;
-    const int bin = border_bin(s, need, wave, lane, before);
+    const int bin = border_bin<LDS::bins>(s, need, wave, lane, before);
     // one pass collects the tokens of the border's step and sums those before it
     const float first = (float)bin;
     uint64_t some = 0;
