@@ -79,7 +79,7 @@ EPIC_DEV float of_key(uint32_t k) {
 }
 
 template <int DT>
-constexpr float kLowest = DT == EPIC_F16 ? -65504.f : -3.38e38f;
+constexpr float kLowest = DT == EPIC_F16 ? -65504.f : DT == EPIC_BF16 ? -0x1.FEp127f : -0x1.FFFFFEp127f;  // finite
 
 // A row read from memory by a pass; wavefronts have the same ids as the lanes
 // that hold it in registers.

@@ -154,6 +154,28 @@ def test_settings_at_their_ends(epic):
             assert tok[b, i] == want[0] and abs(conf[b, i] - want[1]) <= 4e-7 * want[1], (T, k, p, q, u, want)
 
 
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_masks_of_the_lowest_value_at_huge_temperatures(epic, dt):
+    """There they weigh as much as the others, and count for every filter."""
+    V, rng = 700, np.random.default_rng(12)
+    l = np.full(V, torch.finfo(DT[dt]).min)
+    l[rng.permutation(V)[:5]] = [0.0, 1.0, 2.0, 3.0, -1.0]
+    combos = [(T, k, p, q) for T in (1e38, math.inf) for k, p, q in
+              [(0, 1.0, 0.0), (50, 1.0, 0.0), (500, 1.0, 0.0), (0, 0.5, 0.0), (60, 0.9, 0.0), (0, 1.0, 0.01)]]
+    us = np.array([0.0, 0.3, 0.7, 1 - 2.0 ** -24])
+    logits = on(l, torch.float32).to(DT[dt]).expand(len(combos), len(us), V)
+    T, k, p, q = zip(*combos)
+    tok, conf = run(epic, logits, u=np.broadcast_to(us, (len(combos), len(us))), T=T, k=k, p=p, q=q)
+    tok, conf = tok.cpu().numpy(), conf.cpu().numpy()
+    row = logits[0, 0].float().cpu().numpy()
+    for b, (T, k, p, q) in enumerate(combos):
+        T, p, q = np.float32(T), np.float32(p), np.float32(q)
+        e = torch.exp2(torch.from_numpy(R.exponents(row, T)).to(DEV)).cpu().numpy()
+        for i, u in enumerate(us):
+            want = R.draw(row, e, u, T, k, p, q)
+            assert tok[b, i] == want[0] and abs(conf[b, i] - want[1]) <= 4e-7 * want[1], (T, k, p, q, u, want)
+
+
 def test_windows_and_masks(epic):
     """Only masked positions inside the sequence count; what the others hold is
     not looked at."""
