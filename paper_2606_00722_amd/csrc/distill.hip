@@ -89,14 +89,13 @@ EPIC_DEV float teacher_shares(const Entries& e, int K, bool has_lse, float lse, 
   bool there = false;
   for (int k = lane; k < K; k += 64) {
     if (e.id[k] < 0) continue;
-    there = true;
+    there = there || has_lse || e.q[k] != -kInf;  // NaN is no absence
     top = fmaxf(top, e.q[k]);
   }
   any = __ballot(there) != 0;
   float base = lse;
   if (!has_lse) {
     top = wave_max(top);
-    any = any && top > -kInf;
     float s = 0.f;
     for (int k = lane; k < K; k += 64)
       if (e.id[k] >= 0) s += expf(e.q[k] - top);
@@ -110,7 +109,8 @@ EPIC_DEV float teacher_shares(const Entries& e, int K, bool has_lse, float lse, 
     s += q;
   }
   s = wave_sum(s);
-  return has_lse ? fmaxf(1.f - s, 0.f) : 0.f;
+  const float left = 1.f - s;
+  return !has_lse || left < 0.f ? 0.f : left;  // NaN stays
 }
 
 // Whether entry k is the first of its id; `twice`: some id is listed twice.
@@ -288,12 +288,12 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
     zs = wave_sum(zs);
     const float lse_top = zt > -kInf || zs != zs ? zb + logf(zs) : -kInf;
     const float both = fmaxf(lse_rest, lse_top);
-    const float lse = both == -kInf ? -kInf : both + logf(expf(lse_rest - both) + expf(lse_top - both));
+    const bool empty = lse_rest == -kInf && lse_top == -kInf;
+    const float lse = empty ? -kInf : both + logf(expf(lse_rest - both) + expf(lse_top - both));
     const bool has = a.teacher_lse != nullptr;
     bool any = false;
     float q_rest = teacher_shares(ent, K, has, has ? a.teacher_lse[r] : 0.f, lane, any);
     if (lse_rest == -kInf) q_rest = 0.f;
-    const bool empty = lse == -kInf;
     float kl = 0.f;
     for (int k = lane; k < K; k += 64) {
       const float q = ent.id[k] >= 0 ? ent.q[k] : 0.f;

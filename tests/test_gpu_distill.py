@@ -162,6 +162,30 @@ def test_ids_outside_the_vocabulary_and_nan(epic):
         assert (g[0, 0] == 0).all() and np.isnan(g[0, 1]).all()
 
 
+def test_nan_reaches_losses_and_gradients(epic):
+    """A NaN among the teacher's logits or the student's is not taken for an
+    absent entry or an empty row."""
+    rng = np.random.default_rng(2)
+    V = 300
+    logits, ids, t, lse = inputs(rng, 1, 3, V, 5, 1.0, "f32")
+    logits = logits.clone()
+    t[0, 0, 1] = np.nan
+    t[0, 1] = np.nan
+    logits[0, 2] = -math.inf
+    left = np.setdiff1d(np.arange(V), ids[0, 2])
+    logits[0, 2, int(left[7])] = math.nan  # the only one above -inf, and not listed
+    for te in (lse, None):
+        loss, stats, grads = call(epic, logits, None, ids, t, te, 1.0, None)
+        assert np.isnan(loss).all() and np.isnan(stats[0, 2]).all()
+        for g in grads:
+            assert all(np.isnan(g[0, i, ids[0, i]]).all() for i in (1, 2))
+            if te is not None:  # an entry's own share, and what is left to the rest
+                others = np.delete(ids[0, 0], 1)
+                assert np.isfinite(g[0, 0, others]).all() and np.isnan(np.delete(g[0, 0], others)).all() and np.isnan(g[0, 1]).all()
+            else:  # every share of the softmax
+                assert np.isnan(g[0, 0, ids[0, 0]]).all()
+
+
 def test_gradient_against_differences(epic):
     """Differences of the loss in 64 bits at the kernel's float32 inputs."""
     rng = np.random.default_rng(21)
