@@ -1,6 +1,8 @@
 // Proposals from a denoiser's logits: epic_sample and epic_propose.
 #include "rows.inc"
 
+#include <type_traits>
+
 namespace epic_rows {
 
 // ---------------------------------------------------------------- sampling
@@ -36,6 +38,7 @@ struct SampleArgs {
   const int32_t* top_k;
   int32_t* tok;
   float* conf;
+  int spread;  // of how many rows those that count are dealt to the first workgroups (0: to their own)
 };
 
 // floor(mass * part / 2^24) for part <= 2^24
@@ -125,18 +128,18 @@ struct Row {
   }
 };
 
-constexpr int kList = 256;  // tokens that are put in order in LDS
-
-// BINS: of the histogram.  A step in which a border lies should hold no more
-// than kList tokens: 33 doublings of weight in 1024 steps put 90 of 32768
-// normally distributed logits (deviation 2) in one, so rows of more registers
-// have more.
-template <int BINS>
+// BINS: of the histogram, ROOM: of the list, the tokens that are put in order in
+// LDS.  A step in which a border lies should hold no more than ROOM tokens: 33
+// doublings of weight in 1024 steps put 90 of 32768 normally distributed logits
+// (deviation 2) in one, so longer rows have more steps.  That does not part
+// equal logits, of which 131072 in bfloat16 have hundreds of a value: rows that
+// take a CU for themselves have a longer list.
+template <int BINS, int ROOM>
 struct SampleLds {
-  static constexpr int bins = BINS;
+  static constexpr int bins = BINS, room = ROOM;
   static constexpr int skew = BINS + BINS / 16;  // 17 words of 8 bytes every 16 bins
   uint64_t hist[skew];
-  uint64_t list[kList];  // entries, in no order
+  uint64_t list[ROOM];  // entries, in no order
   uint64_t mass[kMaxWaves];
   float top[kMaxWaves];
   int listed;
@@ -543,10 +546,25 @@ EPIC_DEV float bound_of_top(LDS& s, float mine, float mine2, int wave, int waves
 template <int DT, class LDS>
 EPIC_DEV void list_token(LDS& s, float l, int id) {
   const int i = atomicAdd(&s.listed, 1);
-  if (i < kList) s.list[i] = entry(key_of<DT>(l), id);
+  if (i < LDS::room) s.list[i] = entry(key_of<DT>(l), id);
 }
 
-// The entry among the `count` <= kList tokens of s.list at which the
+// Those of a vector's tokens that reach `low`; false once the list is too short.
+template <int DT, class LDS>
+EPIC_DEV bool list_vector(LDS& s, const Vec& x, int id, float low) {
+  uint32_t in = 0;
+#pragma unroll
+  for (int e = 0; e < kPer<DT>; ++e) in |= elem<DT>(x, e) >= low ? 1u << e : 0u;
+  if (!in) return true;
+  int at = atomicAdd(&s.listed, __popc(in));
+  if (at + __popc(in) > LDS::room) return false;
+#pragma unroll
+  for (int e = 0; e < kPer<DT>; ++e)
+    if (in & (1u << e)) s.list[at++] = entry(key_of<DT>(elem<DT>(x, e)), id + e);
+  return true;
+}
+
+// The entry among the `count` <= LDS::room tokens of s.list at which the
 // running sum of their numbers or weights reaches target >= 1; by the whole
 // workgroup, of which one wavefront works.
 template <int DT, bool MASS, class LDS>
@@ -555,13 +573,8 @@ EPIC_DEV uint64_t border_entry(LDS& s, int count, uint64_t target, int wave, int
     auto weigh = [&](uint64_t e) -> uint32_t {
       return e == 0 ? 0u : MASS ? weight(of_key<DT>(key_in(e)), M, c) : 1u;
     };
-    uint64_t cut;
-    if (count <= 64) {
-      const uint64_t ranked = sort64(lane < count ? s.list[lane] : 0);
-      const uint64_t reach = __ballot(scan64(weigh(ranked)) >= target);
-      cut = lane64(ranked, __ffsll((unsigned long long)reach) - 1);
-    } else {
-      constexpr int R = kList / 64;
+    auto search = [&](auto per) {
+      constexpr int R = decltype(per)::value;
       uint64_t e[R];
       uint32_t w[R];
 #pragma unroll
@@ -569,7 +582,17 @@ EPIC_DEV uint64_t border_entry(LDS& s, int count, uint64_t target, int wave, int
         e[r] = r * 64 + lane < count ? s.list[r * 64 + lane] : 0;
         w[r] = weigh(e[r]);
       }
-      cut = reach_entry<DT, MASS>(e, w, target, V);
+      return reach_entry<DT, MASS>(e, w, target, V);
+    };
+    uint64_t cut;
+    if (count <= 64) {
+      const uint64_t ranked = sort64(lane < count ? s.list[lane] : 0);
+      const uint64_t reach = __ballot(scan64(weigh(ranked)) >= target);
+      cut = lane64(ranked, __ffsll((unsigned long long)reach) - 1);
+    } else if (LDS::room == 256 || count <= 256) {
+      cut = search(std::integral_constant<int, 4>());
+    } else {
+      cut = search(std::integral_constant<int, LDS::room / 64>());
     }
     if (lane == 0) s.cut = cut;
   }
@@ -614,7 +637,7 @@ EPIC_DEV uint64_t border_of(const Row<DT>& row, LDS& s, int wave, int waves, flo
     __syncthreads();
     const int count = s.listed;
     __syncthreads();
-    if (count <= kList) return border_entry<DT, MASS>(s, count, target - before, wave, lane, row.V, M, c);
+    if (count <= LDS::room) return border_entry<DT, MASS>(s, count, target - before, wave, lane, row.V, M, c);
   }
   float cut_l = old_l;
   int cut_id = old_id;
@@ -622,15 +645,51 @@ EPIC_DEV uint64_t border_of(const Row<DT>& row, LDS& s, int wave, int waves, flo
   return cut_l == -kInf ? 0 : entry(key_of<DT>(cut_l), cut_id);
 }
 
+// Row number x of all, those that count first and then the others, by the whole
+// workgroup.  Rows that take a CU for themselves and are not many more than the
+// CUs would else lie unevenly: workgroups go to the XCDs and their parts in
+// turn, whether their row counts or not.  1055 rows of 100003 float32 logits of
+// which 158 count, top-p 0.95: 67 us against 105; 1024 of 131072 float16, 212
+// count: 66 against 110.  Where all rows count it costs (1024 rows of 65536
+// bfloat16: 36.0 us without filters against 32.7, 136 with top-p against 134),
+// and the positions of a window are mostly masked: calls with d_start do without.
+constexpr int kSpread = 2048;  // rows at most
+EPIC_DEV int nth_row(const SampleArgs& a, uint64_t* masks, int x, int wave, int waves, int lane) {
+  const int chunks = (a.spread + 63) >> 6;
+  for (int c = wave; c < chunks; c += waves) {
+    const int r = c * 64 + lane, b = r / a.rows;
+    const uint64_t in = __ballot(r < a.spread && row_counts(a.win, b, r - b * a.rows));
+    if (lane == 0) masks[c] = in;
+  }
+  __syncthreads();
+  uint64_t mine = lane < chunks ? masks[lane] : 0;
+  uint64_t upto = scan64((uint64_t)__popcll((unsigned long long)mine));
+  const int all = (int)lane64(upto, 63);
+  if (x >= all) {
+    x -= all;
+    const int left = a.spread - lane * 64;
+    mine = left <= 0 ? 0 : ~mine & (left < 64 ? (1ull << left) - 1 : ~0ull);
+    upto = scan64((uint64_t)__popcll((unsigned long long)mine));
+  }
+  const int c = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot((int)upto > x)) - 1);
+  const uint64_t in = lane64(mine, c);
+  x -= (int)lane64(upto, c) - __popcll((unsigned long long)in);
+  const bool here = (in >> lane & 1) && __popcll((unsigned long long)(in & ((1ull << lane) - 1))) == x;
+  return c * 64 + __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(here)) - 1);
+}
+
 template <int DT, int J>
 __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
-  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024>;
+  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024, J == 0 || J == 16 ? 512 : 256>;
   __shared__ LDS s;
   constexpr int E = kPer<DT>;
   constexpr float kSteps = -(float)(LDS::bins / 33);  // steps of a doubling
-  const int r = (int)blockIdx.x, b = r / a.rows, i = r - b * a.rows;
   const int threads = (int)blockDim.x, waves = threads >> 6;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  int r = (int)blockIdx.x;
+  if constexpr (J == 0 || J == 16)
+    if (a.spread) r = nth_row(a, s.list, r, wave, waves, (int)threadIdx.x & 63);
+  const int b = r / a.rows, i = r - b * a.rows;
   const bool counts = row_counts(a.win, b, i);
   const float T = a.temperature ? a.temperature[b] : 1.0f;
   if (!counts || T != T) {
@@ -681,10 +740,12 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
   };
 
   float mine = -kInf, mine2 = -kInf;  // of the lane's even and odd vectors
+  float largest[J ? J / 2 : 1];       // of every pair of vectors
   each([&](const Vec& x, int j) {
     float m = -kInf;
 #pragma unroll
     for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
+    if constexpr (J > 0) largest[j / 2] = j & 1 ? fmaxf(largest[j / 2], m) : m;
     if (j & 1)
       mine2 = fmaxf(mine2, m);
     else
@@ -828,7 +889,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
     if (lane == 0) s.mass[wave] = some;
     const int count = s.listed;
     __syncthreads();
-    if (count <= kList) {
+    if (count <= LDS::room) {
       cut = border_entry<DT, true>(s, count, need - before, wave, lane, a.V, M, c);
       // the border's own, to the wavefront that has their ids
       for (int i = (int)threadIdx.x; i < count; i += threads) {
@@ -854,24 +915,37 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
     if (!by_k || k <= 2 * threads) {
       if (threadIdx.x == 0) s.listed = 0;
       __syncthreads();
-      if (M_wave >= low) row.vectors([&](const Vec& x, int j) {
-        float m = -kInf;
+      if constexpr (J > 0) {
+        // The lane's pairs of vectors that have one, mostly none, are read again.
+        uint32_t hits = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
-        if (m < low || __hip_atomic_load(&s.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kList) return;
+        for (int j = 0; j < J / 2; ++j) hits |= largest[j] >= low ? 1u << j : 0u;
+        while (hits) {
+          const int j = 2 * (__ffs(hits) - 1), at = row.first + j * 64 + lane;
+          hits &= hits - 1;
+          const Vec x = load_vec<DT>(row.base, at, a.V), y = load_vec<DT>(row.base, at + 64, a.V);
+          if (!list_vector<DT>(s, x, row.id(j), low) || !list_vector<DT>(s, y, row.id(j + 1), low)) break;
+        }
+      } else if (M_wave >= low) {
+        bool open = true;
+        row.vectors([&](const Vec& x, int j) {
+          float m = -kInf;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (elem<DT>(x, e) >= low) list_token<DT>(s, elem<DT>(x, e), row.id(j) + e);
-      });
+          for (int e = 0; e < E; ++e) m = fmaxf(m, elem<DT>(x, e));
+          if (open && m >= low) open = list_vector<DT>(s, x, row.id(j), low);
+        });
+      }
       __syncthreads();
       const int N = __builtin_amdgcn_readfirstlane(s.listed);
-      if (N <= kList) {
+      if (N <= LDS::room) {
         if (wave != 0) return;
         const Draw draw{M, c, k, P, least, U, a.V};
         if (N <= 64)
           draw_from_list<DT, 1>(s.list, N, lane, draw, found);
+        else if (LDS::room == 256 || N <= 256)
+          draw_from_list<DT, 4>(s.list, N, lane, draw, found);
         else
-          draw_from_list<DT, kList / 64>(s.list, N, lane, draw, found);
+          draw_from_list<DT, LDS::room / 64>(s.list, N, lane, draw, found);
         return;
       }
       __syncthreads();
@@ -1128,8 +1202,9 @@ epic_status epic_sample(const epic_rows_desc* logits, const int32_t* d_seqs, int
   if (!d_uniform || !d_tok || !d_conf) return EPIC_ERR_NULL;
   const int es = elem_size(logits->dtype);
   SampleArgs a{(const char*)logits->data, logits->seq_stride * es, logits->row_stride * es, logits->rows, logits->vocab,
-               {d_seqs, d_start, n}, d_uniform, d_temperature, d_top_p, d_min_p, d_top_k, d_tok, d_conf};
+               {d_seqs, d_start, n}, d_uniform, d_temperature, d_top_p, d_min_p, d_top_k, d_tok, d_conf, 0};
   const int blocks = logits->batch * logits->rows;
+  if (d_seqs && !d_start && blocks > 256 && blocks <= kSpread) a.spread = blocks;
   switch (logits->dtype) {
     case EPIC_F32: return launch_sample<EPIC_F32>(a, blocks, stream);
     case EPIC_F16: return launch_sample<EPIC_F16>(a, blocks, stream);

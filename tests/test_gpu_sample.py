@@ -199,6 +199,28 @@ def test_windows_and_masks(epic):
         check_rows(logits[b, i:i + 1], u[b, i:i + 1], np.float32(0.8), 40, 1.0, 0.0, tok[b, i:i + 1], conf[b, i:i + 1], V)
 
 
+@pytest.mark.parametrize("dt,B,m,V", [("bf16", 3, 100, 40001), ("bf16", 300, 1, 140001), ("f32", 7, 37, 40001), ("f16", 1, 2048, 33001),
+                                      ("f16", 1, 2049, 33001)])
+def test_long_rows_of_which_some_count(epic, dt, B, m, V):
+    """The same tokens as a call on these rows alone, and no others touched."""
+    rng = np.random.default_rng(V + m)
+    logits = torch.randn((B, m, V), device=DEV, generator=torch.Generator(DEV).manual_seed(V)).to(DT[dt])
+    u = rng.random((B, m)).astype(np.float32)
+    for masked in (0.0, 0.07, 0.9, 1.0):
+        seqs = np.where(rng.random((B, m + 3)) < masked, -1, 9).astype(np.int32)
+        counts = seqs[:, :m] == -1
+        tok, conf = run(epic, logits, on(seqs, torch.int32), u=u, T=0.9, k=100, p=0.9)
+        tok, conf = tok.cpu().numpy(), conf.cpu().numpy()
+        assert (tok[~counts] == -1).all() and (conf[~counts] == 0).all()
+        rows = np.flatnonzero(counts.reshape(-1))[:200]  # at most 200: a call whose rows stay where they are
+        if len(rows):
+            some = logits.view(-1, V)[on(rows, torch.int64)][None]
+            one = run(epic, some, u=u.reshape(1, -1)[:, rows], T=0.9, k=100, p=0.9)
+            assert (one[0][0].cpu().numpy() == tok.reshape(-1)[rows]).all()
+            assert (one[1][0].cpu().numpy() == conf.reshape(-1)[rows]).all()
+        assert (tok[counts] >= 0).all()
+
+
 def test_a_row_draws_the_same_in_any_batch(epic):
     V, rng = 5003, np.random.default_rng(4)
     logits = torch.from_numpy((2 * rng.standard_normal((6, 9, V))).astype(np.float32)).to(DEV, torch.bfloat16)
