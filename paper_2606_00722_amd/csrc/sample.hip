@@ -1,8 +1,6 @@
 // Proposals from a denoiser's logits: epic_sample and epic_propose.
 #include "rows.inc"
 
-#include <type_traits>
-
 namespace epic_rows {
 
 // ---------------------------------------------------------------- sampling
@@ -140,6 +138,7 @@ struct SampleLds {
   static constexpr int skew = BINS + BINS / 16;  // 17 words of 8 bytes every 16 bins
   uint64_t hist[skew];
   uint64_t list[ROOM];  // entries, in no order
+  uint32_t weights[ROOM];
   uint64_t mass[kMaxWaves];
   float top[kMaxWaves];
   int listed;
@@ -414,44 +413,140 @@ EPIC_DEV int id_in(uint64_t e) { return (int)~(uint32_t)e; }
 // the highest bit of an id
 EPIC_DEV int top_bit(int V) { return V > 1 ? 1 << (31 - __clz(V - 1)) : 0; }
 
-// Sum over a wavefront: of numbers of entries by ballots, of weights by lanes.
-template <bool MASS, int R, class P>
-EPIC_DEV uint64_t sum_where(const uint32_t (&w)[R], P&& is) {
-  uint64_t sum = 0;
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if constexpr (MASS)
-      sum += is(r) ? w[r] : 0u;
-    else
-      sum += (uint64_t)__popcll((unsigned long long)__ballot(is(r)));
-  }
-  return MASS ? wave_sum64(sum) : sum;
+// What the lanes of a wavefront wrote to LDS, before others of its lanes read it.
+EPIC_DEV void lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// The entry at which the running sum of the weights, in the order of the
-// entries, reaches `target` >= 1 (MASS false: their number does), by one
-// wavefront that holds R entries a lane (0: none, of weight 0).  0 when the
-// sum does not reach it.  A search for the key bit by bit, then for the id
-// among equal keys, whose weights are equal too.
-template <int DT, bool MASS, int R>
-EPIC_DEV uint64_t reach_entry(const uint64_t (&e)[R], const uint32_t (&w)[R], uint64_t target, int V) {
-  uint32_t key = 0;
+// Lists in LDS (s.list, entries in no order), worked on by one wavefront.  Sums
+// over the entries i of a list are of part(i).
+template <class P>
+EPIC_DEV uint64_t sum_list(int N, int lane, P&& part) {
+  uint64_t sum = 0;
 #pragma unroll 1
-  for (uint32_t bit = DT == EPIC_F32 ? 0x80000000u : 0x8000u; bit; bit >>= 1) {
-    const uint32_t at = key | bit;
-    if (sum_where<MASS>(w, [&](int r) { return key_in(e[r]) >= at; }) >= target) key = at;
+  for (int i = lane; i < N; i += 64) sum += part(i);
+  return wave_sum64(sum);
+}
+
+// Where the running sum of part(i) reaches `target` >= 1, over the entries in
+// the order of step(i) (0 to 511) and, within a step, of rank(i), greatest
+// first.  Returns the rank of the entry that reaches it; 0 when the sum does not
+// reach it, or when more than 64 entries are in its step, with crowded = true.
+//
+// A histogram over the steps and a sort of the entries of one: a few hundred
+// clocks, where a search for the key bit by bit takes as many for every bit.
+template <class LDS, class S, class K, class P>
+EPIC_DEV uint64_t reach_by_steps(LDS& s, int N, int lane, uint64_t target, S&& step, K&& rank, P&& part,
+                                 bool& crowded) {
+  constexpr int bins = 512;
+  crowded = false;
+#pragma unroll 1
+  for (int i = lane; i < bins + bins / 16; i += 64) s.hist[i] = 0;
+  lds_fence();
+#pragma unroll 1
+  for (int i = lane; i < N; i += 64) {
+    const uint64_t p = part(i);
+    if (p) atomicAdd((unsigned long long*)&s.hist[slot(step(i))], (unsigned long long)p);
   }
-  const uint64_t above = sum_where<MASS>(w, [&](int r) { return key_in(e[r]) > key; });
-  const uint64_t equal = sum_where<MASS>(w, [&](int r) { return e[r] != 0 && key_in(e[r]) == key; });
-  if (above + equal < target) return 0;
-  if (above + equal == target) return entry(key, INT32_MAX);
-  int id = 0;
+  lds_fence();
+  uint64_t before, inside;
+  const int bin = scan_bins<bins>(s.hist, target, lane, before, inside);
+  if (bin < 0) return 0;
+  lds_fence();
+  int count = 0;  // of the step's entries, whose numbers go to the histogram's place
+#pragma unroll 1
+  for (int i0 = 0; i0 < N; i0 += 64) {
+    const int i = i0 + lane;
+    const bool in = i < N && step(i) == bin && part(i) != 0;
+    const uint64_t all = __ballot(in);
+    const int to = count + __popcll((unsigned long long)(all & ((1ull << lane) - 1)));
+    if (in && to < 64) s.hist[to] = (uint64_t)i;
+    count += __popcll((unsigned long long)all);
+  }
+  lds_fence();
+  if (count > 64) {
+    crowded = true;
+    return 0;
+  }
+  const int mine = lane < count ? (int)s.hist[lane] : 0;
+  const uint64_t key = lane < count ? rank(mine) : 0, p = lane < count ? part(mine) : 0;
+  lds_fence();
+  // the parts in the order of the ranks, by the place of every entry in it
+  const uint64_t ranked = sort64(key);
+  int place = 0;
+#pragma unroll 1
+  for (int i = 0; i < count; ++i) place += lane64(ranked, i) > key ? 1 : 0;
+  if (lane < count) s.hist[place] = p;
+  lds_fence();
+  const uint64_t upto = scan64(lane < count ? s.hist[lane] : 0);
+  const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(upto >= target - before)) - 1);
+  return lane64(ranked, j);
+}
+
+// The lowest id at which the running sum of part(i), in the order of the ids,
+// reaches `target` >= 1, into `id` (false: it does not).  If more than 64 are in
+// one of the steps of the vocabulary, bit by bit.
+template <class LDS, class P>
+EPIC_DEV bool reach_id(LDS& s, int N, int lane, uint64_t target, int V, P&& part, int& id) {
+  const float scale = 511.0f / (float)V;
+  bool crowded;
+  const uint64_t e = reach_by_steps(
+      s, N, lane, target, [&](int i) { return (int)((float)id_in(s.list[i]) * scale); },
+      [&](int i) { return (uint64_t)(uint32_t)s.list[i]; }, part, crowded);  // the id's complement
+  id = id_in(e);
+  if (!crowded) return e != 0;
+  if (sum_list(N, lane, part) < target) return false;
+  id = 0;
 #pragma unroll 1
   for (int bit = top_bit(V); bit; bit >>= 1) {
-    const int at = id + bit;
-    if (above + sum_where<MASS>(w, [&](int r) { return key_in(e[r]) == key && id_in(e[r]) < at; }) < target) id = at;
+    const int to = id + bit;
+    if (sum_list(N, lane, [&](int i) { return id_in(s.list[i]) < to ? part(i) : 0; }) < target) id = to;
   }
-  return entry(key, id);
+  return true;
+}
+
+// The entry of s.list at which the running sum of part(i), in the order of the
+// entries, reaches `target` >= 1 (0: it does not).  Steps are even in the logit;
+// if too many entries are in one (equal logits), the key is searched by halves,
+// then the id among equal keys.
+template <int DT, class LDS, class P>
+EPIC_DEV uint64_t reach_entry(LDS& s, int N, int lane, uint64_t target, int V, P&& part) {
+  float top = -kInf, bottom = kInf;
+#pragma unroll 1
+  for (int i = lane; i < N; i += 64) {
+    const float l = of_key<DT>(key_in(s.list[i]));
+    top = fmaxf(top, l);
+    bottom = fminf(bottom, l);
+  }
+  top = wave_max(top);
+  bottom = -wave_max(-bottom);
+  const float scale = 511.0f / (top - bottom);
+  if (scale > 1e-30f && scale < 1e30f) {
+    bool crowded;
+    const uint64_t e = reach_by_steps(
+        s, N, lane, target,
+        [&](int i) { return min((int)((top - of_key<DT>(key_in(s.list[i]))) * scale), 511); },
+        [&](int i) { return s.list[i]; }, part, crowded);
+    if (!crowded) return e;
+  }
+  uint32_t key = key_of<DT>(bottom), over = key_of<DT>(top) + 1;  // the sum is reached at key, if at all, and not at over
+#pragma unroll 1
+  while (over - key > 1) {
+    const uint32_t at = key + (over - key) / 2;
+    if (sum_list(N, lane, [&](int i) { return key_in(s.list[i]) >= at ? part(i) : 0; }) >= target)
+      key = at;
+    else
+      over = at;
+  }
+  const uint64_t above = sum_list(N, lane, [&](int i) { return key_in(s.list[i]) > key ? part(i) : 0; });
+  auto equal = [&](int i) -> uint64_t { return key_in(s.list[i]) == key ? part(i) : 0; };
+  const uint64_t with = above + sum_list(N, lane, equal);
+  if (with < target) return 0;
+  if (with == target) return entry(key, INT32_MAX);
+  int at;
+  const uint64_t found = reach_id(s, N, lane, target - above, V, equal, at);
+  return found ? entry(key, at) : 0;
 }
 
 struct Draw {
@@ -464,61 +559,50 @@ struct Draw {
 };
 
 // The token drawn from a list of N tokens, in which all that the filters can
-// keep are found; by one wavefront, R tokens a lane.
-template <int DT, int R, class F>
-EPIC_DEV void draw_from_list(const uint64_t* list, int N, int lane, const Draw& d, F&& found) {
-  uint64_t e[R];
-  uint32_t w[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    e[r] = r * 64 + lane < N ? list[r * 64 + lane] : 0;
-    w[r] = e[r] ? weight(of_key<DT>(key_in(e[r])), d.M, d.c) : 0;
-  }
+// keep are found; by one wavefront.  Up to 64: a token a lane.
+template <int DT, class LDS, class F>
+EPIC_DEV void draw_from_short_list(LDS& s, int N, int lane, const Draw& d, F&& found) {
+  const uint64_t e = lane < N ? s.list[lane] : 0;
+  uint32_t w = e ? weight(of_key<DT>(key_in(e)), d.M, d.c) : 0;
   uint64_t cut = 0;
-  if constexpr (R == 1) {  // in order, a token a lane
-    if (d.k < N || d.P < 16777216u) {
-      const uint64_t ranked = sort64(e[0]);
-      const uint64_t rw = ranked && lane < d.k ? (uint64_t)weight(of_key<DT>(key_in(ranked)), d.M, d.c) : 0;
-      const uint64_t upto = scan64(rw);
-      const uint64_t want = share(lane64(upto, 63), d.P), need = want > 0 ? want : 1;
-      // the tokens whose mass before is short of the need: a prefix of the order
-      const uint64_t prefix = __ballot(ranked != 0 && lane < d.k && upto - rw < need);
-      cut = lane64(ranked, 63 - __clzll((long long)(prefix | 1)));
-    }
-  } else {
-    if (d.k < N) {
-      cut = reach_entry<DT, false>(e, w, (uint64_t)d.k, d.V);
-    }
-    if (d.P < 16777216u) {
-      uint32_t in[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) in[r] = e[r] >= cut ? w[r] : 0;
-      const uint64_t sum = sum_where<true>(in, [&](int) { return true; });
-      const uint64_t want = share(sum, d.P), need = want > 0 ? want : 1;
-      if (need < sum) cut = reach_entry<DT, true>(e, in, need, d.V);
-    }
+  if (d.k < N || d.P < 16777216u) {
+    const uint64_t ranked = sort64(e);
+    const uint64_t rw = ranked && lane < d.k ? (uint64_t)weight(of_key<DT>(key_in(ranked)), d.M, d.c) : 0;
+    const uint64_t upto = scan64(rw);
+    const uint64_t want = share(lane64(upto, 63), d.P), need = want > 0 ? want : 1;
+    // the tokens whose mass before is short of the need: a prefix of the order
+    const uint64_t prefix = __ballot(ranked != 0 && lane < d.k && upto - rw < need);
+    cut = lane64(ranked, 63 - __clzll((long long)(prefix | 1)));
   }
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (e[r] < cut || w[r] < d.least) w[r] = 0;
-  int id;
-  if constexpr (R == 1) {  // in the order of the ids, the weights with them
-    const uint64_t by_id = sort64(w[0] ? ((uint64_t)(uint32_t)e[0] << 32) | w[0] : 0);
-    const uint64_t upto = scan64((uint32_t)by_id);
-    const uint64_t here = __ballot(upto > share(lane64(upto, 63), d.U));
-    id = ~__builtin_amdgcn_readlane((int)(by_id >> 32), __ffsll((unsigned long long)here) - 1);
-  } else {  // the last id below which the mass is not over the target
-    const uint64_t target = share(sum_where<true>(w, [&](int) { return true; }), d.U);
-    id = 0;
+  if (e < cut || w < d.least) w = 0;
+  // in the order of the ids, the weights with them
+  const uint64_t by_id = sort64(w ? ((uint64_t)(uint32_t)e << 32) | w : 0);
+  const uint64_t upto = scan64((uint32_t)by_id);
+  const uint64_t here = __ballot(upto > share(lane64(upto, 63), d.U));
+  const int id = ~__builtin_amdgcn_readlane((int)(by_id >> 32), __ffsll((unsigned long long)here) - 1);
+  if (w && id_in(e) == id) found(id, of_key<DT>(key_in(e)));
+}
+template <int DT, class LDS, class F>
+EPIC_DEV void draw_from_list(LDS& s, int N, int lane, const Draw& d, F&& found) {
 #pragma unroll 1
-    for (int bit = top_bit(d.V); bit; bit >>= 1) {
-      const int at = id + bit;
-      if (sum_where<true>(w, [&](int r) { return id_in(e[r]) < at; }) <= target) id = at;
-    }
+  for (int i = lane; i < N; i += 64) s.weights[i] = weight(of_key<DT>(key_in(s.list[i])), d.M, d.c);
+  lds_fence();
+  uint64_t cut = 0;
+  if (d.k < N) cut = reach_entry<DT>(s, N, lane, (uint64_t)d.k, d.V, [&](int) -> uint64_t { return 1; });
+  if (d.P < 16777216u) {
+    auto in = [&](int i) -> uint64_t { return s.list[i] >= cut ? s.weights[i] : 0; };
+    const uint64_t sum = sum_list(N, lane, in);
+    const uint64_t want = share(sum, d.P), need = want > 0 ? want : 1;
+    if (need < sum) cut = reach_entry<DT>(s, N, lane, need, d.V, in);
   }
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (w[r] && id_in(e[r]) == id) found(id, of_key<DT>(key_in(e[r])));
+  auto kept = [&](int i) -> uint64_t { return s.list[i] >= cut && s.weights[i] >= d.least ? s.weights[i] : 0; };
+  // the lowest id at which the mass is over the target
+  const uint64_t target = share(sum_list(N, lane, kept), d.U);
+  int id;
+  if (!reach_id(s, N, lane, target + 1, d.V, kept, id)) return;  // the kept mass is 2^31 at least
+#pragma unroll 1
+  for (int i = lane; i < N; i += 64)
+    if (id_in(s.list[i]) == id) found(id, of_key<DT>(key_in(s.list[i])));
 }
 
 // A logit that at least k of the lanes' largest of their even and odd vectors
@@ -573,26 +657,16 @@ EPIC_DEV uint64_t border_entry(LDS& s, int count, uint64_t target, int wave, int
     auto weigh = [&](uint64_t e) -> uint32_t {
       return e == 0 ? 0u : MASS ? weight(of_key<DT>(key_in(e)), M, c) : 1u;
     };
-    auto search = [&](auto per) {
-      constexpr int R = decltype(per)::value;
-      uint64_t e[R];
-      uint32_t w[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        e[r] = r * 64 + lane < count ? s.list[r * 64 + lane] : 0;
-        w[r] = weigh(e[r]);
-      }
-      return reach_entry<DT, MASS>(e, w, target, V);
-    };
     uint64_t cut;
     if (count <= 64) {
       const uint64_t ranked = sort64(lane < count ? s.list[lane] : 0);
       const uint64_t reach = __ballot(scan64(weigh(ranked)) >= target);
       cut = lane64(ranked, __ffsll((unsigned long long)reach) - 1);
-    } else if (LDS::room == 256 || count <= 256) {
-      cut = search(std::integral_constant<int, 4>());
     } else {
-      cut = search(std::integral_constant<int, LDS::room / 64>());
+#pragma unroll 1
+      for (int i = lane; i < count; i += 64) s.weights[i] = weigh(s.list[i]);
+      lds_fence();
+      cut = reach_entry<DT>(s, count, lane, target, V, [&](int i) -> uint64_t { return s.weights[i]; });
     }
     if (lane == 0) s.cut = cut;
   }
@@ -680,7 +754,7 @@ EPIC_DEV int nth_row(const SampleArgs& a, uint64_t* masks, int x, int wave, int 
 
 template <int DT, int J>
 __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
-  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024, J == 0 || J == 16 ? 512 : 256>;
+  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024, 512>;
   __shared__ LDS s;
   constexpr int E = kPer<DT>;
   constexpr float kSteps = -(float)(LDS::bins / 33);  // steps of a doubling
@@ -941,11 +1015,9 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
         if (wave != 0) return;
         const Draw draw{M, c, k, P, least, U, a.V};
         if (N <= 64)
-          draw_from_list<DT, 1>(s.list, N, lane, draw, found);
-        else if (LDS::room == 256 || N <= 256)
-          draw_from_list<DT, 4>(s.list, N, lane, draw, found);
+          draw_from_short_list<DT>(s, N, lane, draw, found);
         else
-          draw_from_list<DT, LDS::room / 64>(s.list, N, lane, draw, found);
+          draw_from_list<DT>(s, N, lane, draw, found);
         return;
       }
       __syncthreads();

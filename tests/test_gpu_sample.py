@@ -115,6 +115,33 @@ def test_rows_with_many_equal_logits(epic, dt, kind):
             assert tok[b, i] == want[0] and abs(conf[b, i] - want[1]) <= 4e-7 * want[1], (b, i, want)
 
 
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_lists_with_equal_or_adjacent_tokens(epic, dt):
+    """A few hundred tokens in reach of the filters: many of them equal, or
+    all of adjacent ids in a long row."""
+    rng = np.random.default_rng(17)
+    equal = np.full(3000, -30.0)
+    at = rng.permutation(3000)[:230]
+    equal[at[:50]] = 3.0 + 0.125 * rng.integers(0, 8, 50)
+    equal[at[50:200]] = 2.5
+    equal[at[200:]] = 2.25
+    long = np.full(131072, -40.0)
+    long[70000:70300] = 2.0 + 0.25 * rng.integers(0, 9, 300)
+    combos = [(1.0, k, p, q) for k, p, q in [(40, 1.0, 0.0), (80, 1.0, 0.0), (120, 0.9, 0.0), (200, 0.5, 0.0), (210, 0.99, 0.0),
+                                             (230, 1.0, 0.3), (260, 0.7, 0.0), (0, 0.6, 0.0), (0, 0.97, 0.0), (0, 1.0, 0.2)]]
+    T, k, p, q = zip(*combos)
+    for l in (equal, long):
+        logits = on(l, torch.float32).to(DT[dt]).expand(len(combos), 4, len(l))
+        u = rng.random((len(combos), 4)).astype(np.float32)
+        tok, conf = run(epic, logits, u=u, T=T, k=k, p=p, q=q)
+        tok, conf = tok.cpu().numpy(), conf.cpu().numpy()
+        row = logits[0, 0].float().cpu().numpy()
+        e = torch.exp2(torch.from_numpy(R.exponents(row, np.float32(1.0))).to(DEV)).cpu().numpy()
+        for b, i in np.ndindex(*u.shape):
+            want = R.draw(row, e, float(u[b, i]), np.float32(1.0), k[b], np.float32(p[b]), np.float32(q[b]))
+            assert tok[b, i] == want[0] and abs(conf[b, i] - want[1]) <= 4e-7 * want[1], (len(l), combos[b], i, want)
+
+
 def test_rows_without_a_choice(epic):
     V = 300
     logits = torch.zeros((1, 6, V), device=DEV)
