@@ -340,18 +340,19 @@ def _rows(name, t, device=None) -> _Rows:
     sb, sm, sv = t.stride()
     if sv != 1 and V > 1:
         raise ValueError(f"{name}: a row's logits have to be adjacent, got strides {t.stride()}")
-    if not t.is_cuda or (device is not None and t.device != device):
-        raise ValueError(f"{name}: on {t.device}, needs a GPU tensor" + (f" on {device}" if device else ""))
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise ValueError(f"{name}: on {t.device}, needs a GPU tensor" + ("" if device is None else f" on cuda:{device}"))
     return _Rows(t.data_ptr(), _DTYPES[t.dtype], B, m, V, sb, sm)
 
 
 def _arg(name, t, dtype, shape, device):
-    """The address of a contiguous tensor of that type and shape (None: 0)."""
+    """The address of a contiguous tensor of that type and shape (None: 0) on
+    the GPU of that number: comparing device objects takes twice the time."""
     if t is None:
         return 0
-    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+    if t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name}: contiguous {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
+    raise ValueError(f"{name}: contiguous {dtype} {tuple(shape)} on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
                      + ("" if t.is_contiguous() else ", not contiguous"))
 
 
@@ -370,10 +371,10 @@ def _call(fn, device, stream, *args):
     """The library call on `stream` (default: the device's current one), with
     the tensors' device current."""
     if stream is None:
-        s = _torch._C._cuda_getCurrentRawStream(device.index)  # current_stream() makes an object: 1.7 us against 0.05
+        s = _torch._C._cuda_getCurrentRawStream(device)  # current_stream() makes an object: 1.7 us against 0.05
     else:
         s = stream.cuda_stream
-    if _torch.cuda.current_device() == device.index:
+    if _torch.cuda.current_device() == device:
         code = getattr(_lib, fn)(*args, s)
     else:
         with _torch.cuda.device(device):
@@ -389,7 +390,7 @@ def sample(logits, seqs, uniform, tok, conf, start=None, temperature=None, top_k
     conf float32 [B, m] are written.  Settings per sequence, or None:
     temperature, top_p, min_p float32 [B], top_k int32 [B]; start int32 [B]."""
     rows = _rows("logits", logits)
-    dev, (B, m, _) = logits.device, logits.shape
+    dev, (B, m, _) = logits.get_device(), logits.shape
     i32, f32 = _DTYPES["i32"], _DTYPES["f32"]
     sp, n, st = _window(seqs, start, B, dev)
     if uniform is None or tok is None or conf is None:
@@ -409,7 +410,7 @@ def propose(tok, conf, per_seq, cand_seq, cand_pos, cand_tok, cand_conf, offsets
     i32, f32 = _DTYPES["i32"], _DTYPES["f32"]
     if tok.dim() != 2 or not tok.is_cuda:
         raise ValueError(f"tok: int32 [B, m] on a GPU, got {tuple(tok.shape)} on {tok.device}")
-    dev, (B, m) = tok.device, tok.shape
+    dev, (B, m) = tok.get_device(), tok.shape
     C = (B * per_seq,)
     _call("epic_propose", dev, stream, _arg("tok", tok, i32, (B, m), dev), _arg("conf", conf, f32, (B, m), dev), B, m,
           _arg("start", start, i32, (B,), dev), per_seq, _arg("cand_seq", cand_seq, i32, C, dev),
@@ -418,7 +419,7 @@ def propose(tok, conf, per_seq, cand_seq, cand_pos, cand_tok, cand_conf, offsets
 
 
 def _teacher(logits, top_idx, top_logit, teacher_lse):
-    dev, (B, m, _) = logits.device, logits.shape
+    dev, (B, m, _) = logits.get_device(), logits.shape
     if top_idx.dim() != 3:
         raise ValueError(f"top_idx: int32 [B, m, K], got {tuple(top_idx.shape)}")
     K = top_idx.shape[2]
@@ -436,7 +437,7 @@ def distill_forward(logits, seqs, top_idx, top_logit, loss, stats, start=None, t
     backward pass; with grad (like logits, or logits itself) also the gradient
     of sum(weight * loss), weight float32 [B, m] or None for 1."""
     rows = _rows("logits", logits)
-    dev, (B, m, _) = logits.device, logits.shape
+    dev, (B, m, _) = logits.get_device(), logits.shape
     f32 = _DTYPES["f32"]
     sp, n, st = _window(seqs, start, B, dev)
     ti, tl, K, te = _teacher(logits, top_idx, top_logit, teacher_lse)
@@ -451,7 +452,7 @@ def distill_backward(logits, seqs, top_idx, top_logit, stats, weight, grad, star
     """epic_distill_backward: the gradient of sum(weight * loss) from the stats
     of a distill_forward over the same inputs."""
     rows = _rows("logits", logits)
-    dev, (B, m, _) = logits.device, logits.shape
+    dev, (B, m, _) = logits.get_device(), logits.shape
     f32 = _DTYPES["f32"]
     sp, n, st = _window(seqs, start, B, dev)
     ti, tl, K, te = _teacher(logits, top_idx, top_logit, teacher_lse)
