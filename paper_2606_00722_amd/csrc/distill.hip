@@ -144,6 +144,11 @@ struct DistillLds {
 // as the rest's derivative (0 where it was listed), then the listed ones over
 // it.  The sums and shares are float32 relative to their largest; gradients are
 // rounded once, to the logits' type.
+//
+// Bound by memory: losses and gradient of 2867 of 4096 rows of 32768 bfloat16
+// logits take 103 us, 4.4 TB/s of what has to be read and written (a copy: 5.0);
+// the vector units are busy half of the time.  Losses alone of 936 rows of 50021
+// float16 logits take 33 us, 2.9 TB/s: less than four workgroups a CU in all.
 template <int DT, int J, bool GRAD>
 __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
   extern __shared__ uint32_t dyn[];
@@ -353,7 +358,8 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
 
 // Backward from a forward pass's stats: one workgroup per row, one reading and
 // one writing of it.  Every element goes as one of the rest; then the listed
-// ones are written over.
+// ones are written over.  Bound by memory: 8192 rows of 32768 bfloat16 logits take
+// 222 us, 4.85 TB/s (a copy: 5.0).
 template <int DT>
 __global__ void __launch_bounds__(1024) distill_backward_kernel(DistillArgs a) {
   extern __shared__ uint32_t dyn[];

@@ -11,20 +11,32 @@ namespace epic_rows {
 // filter one wavefront then finds the token.
 //
 // With a filter the tokens that it can keep are few in most rows, and end in a
-// list in LDS in the order of their ids, where one wavefront does the rest:
+// list in LDS, where one wavefront does the rest:
 //  * top-k: those above a bound that follows from the lanes' largest logits;
 //  * top-p: a histogram of the weights over the logits gives the step in which
-//    the mass is reached, and those up to that step are listed;
+//    the mass is reached, and those of that step are listed;
 //  * min-p: those above the logit that it stands for.
-// If the list is too short for them (flat rows), only the tokens of that step
-// are listed; they give the exact border, and one more pass sums what is kept.
-// If even those are too many (thousands of equal logits), the border is found
-// by rounds of ever finer histograms.  The passes after the first two read the
-// row again, from L2: as unrolled code over registers they took as many
-// registers as there are, and their arithmetic costs seven times the reading.
+// For top-k and min-p only the pairs of vectors whose largest logit is above the
+// bound are read again, mostly none of a lane's.  If the list is too short for
+// them (flat rows, a large k), a histogram gives the step of the border, the
+// tokens of that step are listed and give the exact border, and one more pass
+// sums what is kept.  If even those are too many (thousands of equal logits), the
+// border is found by rounds of ever finer histograms.  The passes of top-p after
+// the first read the row again, from L2: as unrolled code over registers they
+// took as many registers as there are, and their arithmetic costs seven times the
+// reading.
 //
 // Weights are whole numbers (2^31 for the likeliest token), so the order of
 // the sums, the atomics' order among them, changes no result.
+//
+// Bound: without filters by the reading and the exponentials, about even (2048
+// rows of 32768 bfloat16 logits, 80 % of them counted, in 32 us: 3.5 TB/s, vector
+// units busy 60 %).  With top-k the list's latency is added (2867 rows, top-k 50:
+// 60 us against 46), with top-p the arithmetic of two more passes (134 us; 23
+// instructions a logit in all).  Few rows are bound by the length of the chain:
+// one row of 32768 takes 7 us without and 10 us with all filters.  Rows of 100003
+// float32 logits are read by every pass: 158 of them with top-p take 60 us, of
+// which four readings at a copy's 5.0 TB/s are 50.
 constexpr float kOne = 2147483648.0f;
 
 struct SampleArgs {
@@ -1067,6 +1079,10 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
 // from how many the earlier sequences have, min(per_seq, rows with a token):
 // every workgroup counts them itself, which is one load of 64 tokens for most
 // sequences; a batch too large for that has them counted by a launch before.
+//
+// Bound by latency: 64 sequences of 1024 positions take 7.7 us on the GPU (0.5 MB,
+// 0.1 us of reading), 8 of 128 take 4.8; the sort of 64 is 21 exchanges, a merge
+// six, and each load of the counting is one trip to memory.
 struct ProposeArgs {
   const int32_t* tok;
   const float* conf;
@@ -1240,17 +1256,18 @@ epic_status launch_sample(const SampleArgs& a, int blocks, hipStream_t stream) {
   const int nvec = (a.V + kPer<DT> - 1) / kPer<DT>;
   auto threads = [&](int J) { return std::max(64, ((nvec + J - 1) / J + 63) / 64 * 64); };
 #define EPIC_SAMPLE(J, NT) hipLaunchKernelGGL((sample_kernel<DT, J>), dim3(blocks), dim3(NT), 0, stream, a)
-  // Eight vectors a lane up to 512 lanes: three workgroups fit a CU.  Sixteen
-  // from there on (2048 rows of 40960 bfloat16 logits 47 us against 55, of
-  // 65536 62 against 85: wider workgroups of eight fit one a CU); at 32768
-  // sixteen take 33 us against 36 without filters, but 2867 rows of mixed
-  // settings 185 against 115, as fewer lanes give a looser bound for top-k.
-  // Four and two for short rows (512 rows of 4096 with top-p 17 us against 25).
+  // Eight vectors a lane up to 768 lanes, which two workgroups of a CU can have:
+  // 2048 rows of 49152 bfloat16 logits with top-p 0.9 154 us against 204 with
+  // sixteen, 2867 of 32768 134 against 171 (46 without filters on either side).
+  // Sixteen from there on: 2048 rows of 50304 with top-k 50 81 us against 103, of
+  // 65536 76 against 106, as one workgroup of eight would take a CU.  Four and two
+  // for short rows: 512 rows of 4096 float16 logits with top-p 0.9 16 us against
+  // 23, with settings of all kinds 28 against 47.
   if (nvec <= 2 * 64)
     EPIC_SAMPLE(2, threads(2));
   else if (nvec <= 4 * 256)
     EPIC_SAMPLE(4, threads(4));
-  else if (nvec <= 8 * 512)
+  else if (nvec <= 8 * 768)
     EPIC_SAMPLE(8, threads(8));
   else if (nvec <= 16 * 1024)
     EPIC_SAMPLE(16, threads(16));

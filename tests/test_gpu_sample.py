@@ -227,7 +227,7 @@ def test_windows_and_masks(epic):
 
 
 @pytest.mark.parametrize("dt,B,m,V", [("bf16", 3, 100, 40001), ("bf16", 300, 1, 140001), ("f32", 7, 37, 40001), ("f16", 1, 2048, 33001),
-                                      ("f16", 1, 2049, 33001)])
+                                      ("f16", 1, 2049, 33001), ("f16", 1, 1500, 60001)])
 def test_long_rows_of_which_some_count(epic, dt, B, m, V):
     """The same tokens as a call on these rows alone, and no others touched."""
     rng = np.random.default_rng(V + m)
