@@ -31,9 +31,9 @@ namespace epic_rows {
 //
 // Bound: without filters by the reading and the exponentials, about even (2048
 // rows of 32768 bfloat16 logits, 80 % of them counted, in 32 us: 3.5 TB/s, vector
-// units busy 60 %).  With top-k the list's latency is added (2867 rows, top-k 50:
-// 60 us against 46), with top-p the arithmetic of two more passes (134 us; 23
-// instructions a logit in all).  Few rows are bound by the length of the chain:
+// units busy half of the time).  With top-k the list's latency is added (2867 rows, top-k 50:
+// 60 us against 46), with top-p the arithmetic of two more passes (134 us;
+// settings of all kinds take 23 vector instructions a logit, none 14).  Few rows are bound by the length of the chain:
 // one row of 32768 takes 7 us without and 10 us with all filters.  Rows of 100003
 // float32 logits are read by every pass: 158 of them with top-p take 60 us, of
 // which four readings at a copy's 5.0 TB/s are 50.
