@@ -1113,40 +1113,76 @@ EPIC_DEV uint64_t merge64(uint64_t a, uint64_t b) {
   return sort_step<64, 32>(a > b ? a : b);
 }
 
-// min(P, rows of sequence b with a token), by one wavefront
+// Adds the rows with a token among 64 H rows from `at` of eight sequences first,
+// first + step, ..., whose loads are all in flight together; counts end at P.
+// True while a sequence has less.
+constexpr int kCounts = 8;
+template <int H>
+EPIC_DEV bool count_round(const ProposeArgs& a, int first, int step, int64_t at, int lane, int (&n)[kCounts]) {
+  int32_t t[kCounts][H];
+  float f[kCounts][H];
+#pragma unroll
+  for (int g = 0; g < kCounts; ++g)
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      // never a branch around a load: they would wait for each other
+      const int64_t i = at + h * 64 + lane;
+      const int64_t from = (int64_t)min(first + g * step, a.B - 1) * a.m + (i < a.m ? i : a.m - 1);
+      t[g][h] = a.tok[from];
+      f[g][h] = a.conf[from];
+    }
+  bool open = false;
+#pragma unroll
+  for (int g = 0; g < kCounts; ++g) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const bool there = at + h * 64 + lane < a.m && first + g * step < a.B;
+      n[g] += __popcll((unsigned long long)__ballot(there && proposes(t[g][h], f[g][h])));
+    }
+    n[g] = min(n[g], a.P);
+    open = open || (n[g] < a.P && first + g * step < a.B);
+  }
+  return open;
+}
+// min(P, rows of sequence b with a token), by one wavefront, 512 rows at a time
 EPIC_DEV int count_rows(const ProposeArgs& a, int b, int lane) {
+  constexpr int G = 8;
+  const int32_t* tok = a.tok + (int64_t)b * a.m;
+  const float* conf = a.conf + (int64_t)b * a.m;
   int n = 0;
-  for (int at = 0; at < a.m && n < a.P; at += 64) {
-    const int i = at + lane;
-    bool yes = false;
-    if (i < a.m) yes = proposes(a.tok[(int64_t)b * a.m + i], a.conf[(int64_t)b * a.m + i]);
-    n += __popcll((unsigned long long)__ballot(yes));
+#pragma unroll 1
+  for (int64_t at = lane; at - lane < a.m && n < a.P; at += 64 * G) {
+    int32_t t[G];
+    float f[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      t[g] = -1;
+      f[g] = 0.f;
+      if (at + g * 64 < a.m) {
+        t[g] = tok[at + g * 64];
+        f[g] = conf[at + g * 64];
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) n += __popcll((unsigned long long)__ballot(proposes(t[g], f[g])));
   }
   return min(n, a.P);
 }
-
-// Eight sequences' counts at once, first, first + step, ...: most are settled by
-// the first 64 rows, whose loads are all in flight together.
-constexpr int kCounts = 8;
+// min(P, rows with a token) of eight sequences, by one wavefront.  Most are settled
+// by their first 64 rows.  Up to 320 rows the others' rest follows at once (64
+// sequences of 300 rows that have fewer than P: 10 us a call against 13 for one
+// sequence after another), longer ones go one by one (64 of 1024: 13 us against 20).
 EPIC_DEV void count_eight(const ProposeArgs& a, int first, int step, int lane, int (&n)[kCounts]) {
-  int32_t t[kCounts];
-  float f[kCounts];
 #pragma unroll
-  for (int g = 0; g < kCounts; ++g) {
-    const int b = first + g * step;
-    t[g] = -1;
-    f[g] = 0.f;
-    if (b < a.B && lane < a.m) {
-      t[g] = a.tok[(int64_t)b * a.m + lane];
-      f[g] = a.conf[(int64_t)b * a.m + lane];
-    }
+  for (int g = 0; g < kCounts; ++g) n[g] = 0;
+  if (a.m <= 0 || !count_round<1>(a, first, step, 0, lane, n) || a.m <= 64) return;
+  if (a.m <= 64 + 256) {
+    count_round<4>(a, first, step, 64, lane, n);
+    return;
   }
 #pragma unroll
-  for (int g = 0; g < kCounts; ++g) {
-    n[g] = min(__popcll((unsigned long long)__ballot(proposes(t[g], f[g]))), a.P);
-    const int b = first + g * step;
-    if (n[g] < a.P && a.m > 64 && b < a.B) n[g] = count_rows(a, b, lane);
-  }
+  for (int g = 0; g < kCounts; ++g)
+    if (n[g] < a.P && first + g * step < a.B) n[g] = count_rows(a, first + g * step, lane);
 }
 
 // the offsets of a large batch: one workgroup, sequences dealt to wavefronts
