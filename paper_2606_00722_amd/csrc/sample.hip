@@ -267,7 +267,7 @@ EPIC_DEV uint32_t last_key(uint32_t lo, uint32_t hi, int lane, P&& holds) {
 template <int BINS, class LDS>
 EPIC_DEV int border_bin(LDS& s, uint64_t target, int wave, int lane, uint64_t& before) {
   if (wave == 0) {
-    uint64_t under, inside;
+    uint64_t under = 0, inside;  // no bin: nothing before
     const int bin = scan_bins<BINS>(s.hist, target, lane, under, inside);
     if (lane == 0) {
       s.id = bin;
@@ -877,11 +877,15 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
     // With it the weights by steps of the exponent, for top-p's border.  What
     // top-p leaves out weighs (1 - p) W at least, and W is 2^31 at least: steps
     // of which no token weighs the V-th part of that are not needed to get there.
+    // A weight is up to 2^31 e + 1/2, and where less than a whole one is left of
+    // that part without the half, no step is left out.  The border's step is then
+    // always found: the steps counted weigh W - (1 - p) 2^31 >= p W.
     for (int i = (int)threadIdx.x; i < LDS::skew; i += threads) s.hist[i] = 0;
     if (threadIdx.x == 0) s.listed = 0;
     __syncthreads();
-    const float light = (float)(16777216u - P) * (1.f / 16777216.f) / (float)a.V;
-    const float last = fminf(floorf(log2f(light) * kSteps) + 2.f, (float)LDS::bins);
+    const float light = (float)(16777216u - P) * (kOne / 16777216.f) / (float)a.V - 0.5f;
+    const float all_steps = (float)LDS::bins;
+    const float last = light > 1.f ? fminf(floorf(log2f(light / kOne) * kSteps) + 2.f, all_steps) : all_steps;
     row.template vectors<4>([&](const Vec& v, int) {
       uint64_t all = 0;
 #pragma unroll
