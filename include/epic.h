@@ -334,7 +334,8 @@ epic_status epic_diag_clock_rates(int32_t* shader_khz, int32_t* wall_khz);
  *
  * data is a device pointer aligned to its element; rows need no more alignment
  * and no particular stride (a stride of 0 repeats a row; the rows of a gradient
- * must not overlap).  1 <= vocab <= 262144, else EPIC_ERR_UNSUPPORTED; offsets
+ * must not overlap).  1 <= vocab <= 262144, else EPIC_ERR_UNSUPPORTED; batch *
+ * rows < 2^30, else EPIC_ERR_ARG (of epic_propose batch * per_seq too); offsets
  * are 64-bit.  batch * rows = 0 is no error.  The calls allocate nothing, keep
  * nothing and may be captured in a HIP graph; the same inputs give the same
  * bits, whatever else is in the batch. */

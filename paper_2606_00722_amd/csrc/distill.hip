@@ -20,6 +20,7 @@ struct DistillArgs {
   const float* weight;
   char* grad;
   int64_t grad_seq, grad_row;  // bytes
+  int first;            // row of the launch
 };
 
 // Vector v of a gradient row, rounded to nearest even; nothing past its end.
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
   extern __shared__ uint32_t dyn[];
   __shared__ DistillLds s;
   constexpr int E = kPer<DT>;
-  const int r = (int)blockIdx.x, b = r / a.rows, i = r - b * a.rows;
+  const int r = a.first + (int)blockIdx.x, b = r / a.rows, i = r - b * a.rows;
   const int tid = (int)threadIdx.x, threads = (int)blockDim.x, waves = threads >> 6, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   char* grow = GRAD ? a.grad + b * a.grad_seq + i * a.grad_row : nullptr;
@@ -365,7 +366,7 @@ __global__ void __launch_bounds__(1024) distill_backward_kernel(DistillArgs a) {
   extern __shared__ uint32_t dyn[];
   __shared__ DistillLds s;
   constexpr int E = kPer<DT>;
-  const int r = (int)blockIdx.x, b = r / a.rows, i = r - b * a.rows;
+  const int r = a.first + (int)blockIdx.x, b = r / a.rows, i = r - b * a.rows;
   const int tid = (int)threadIdx.x, threads = (int)blockDim.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   char* grow = a.grad + b * a.grad_seq + i * a.grad_row;
@@ -438,7 +439,11 @@ void launch_forward(DistillArgs a, int blocks, hipStream_t stream) {
   // Losses alone keep nothing in registers, but deal the row to the lanes alike,
   // so that their bits are those of a call with the gradient.
   a.steps = J ? J : (nvec + NT - 1) / NT;
-#define EPIC_DISTILL(J) hipLaunchKernelGGL((distill_forward_kernel<DT, J, GRAD>), dim3(blocks), dim3(NT), lds, stream, a)
+#define EPIC_DISTILL(J)                                                                                \
+  launches(blocks, NT, [&](int first, int count) {                                                     \
+    a.first = first;                                                                                   \
+    hipLaunchKernelGGL((distill_forward_kernel<DT, J, GRAD>), dim3(count), dim3(NT), lds, stream, a);  \
+  })
   if constexpr (!GRAD) {
     EPIC_DISTILL(0);
   } else {
@@ -454,12 +459,15 @@ void launch_forward(DistillArgs a, int blocks, hipStream_t stream) {
 }
 
 template <int DT>
-void launch_distill(const DistillArgs& a, bool forward, int blocks, hipStream_t stream) {
+void launch_distill(DistillArgs a, bool forward, int blocks, hipStream_t stream) {
   if (!forward) {
     const int nvec = (a.V + kPer<DT> - 1) / kPer<DT>;
     const int threads = std::min(512, std::max(64, (nvec + 255) / 256 * 64));
     const size_t lds = ((size_t)(a.V + 31) / 32 + 3 * (size_t)a.K) * 4;
-    hipLaunchKernelGGL(distill_backward_kernel<DT>, dim3(blocks), dim3(threads), lds, stream, a);
+    launches(blocks, threads, [&](int first, int count) {
+      a.first = first;
+      hipLaunchKernelGGL(distill_backward_kernel<DT>, dim3(count), dim3(threads), lds, stream, a);
+    });
   } else if (a.grad) {
     launch_forward<DT, true>(a, blocks, stream);
   } else {
@@ -487,7 +495,7 @@ epic_status distill(const epic_rows_desc* logits, const int32_t* d_seqs, int32_t
   const int es = elem_size(logits->dtype);
   DistillArgs a{(const char*)logits->data, logits->seq_stride * es, logits->row_stride * es, logits->rows, logits->vocab,
                 {d_seqs, d_start, n}, d_top_idx, d_top_logit, K, 0, d_teacher_lse, tau, d_loss, d_stats, d_weight,
-                grad ? (char*)grad->data : nullptr, grad ? grad->seq_stride * es : 0, grad ? grad->row_stride * es : 0};
+                grad ? (char*)grad->data : nullptr, grad ? grad->seq_stride * es : 0, grad ? grad->row_stride * es : 0, 0};
   const int blocks = logits->batch * logits->rows;
   switch (logits->dtype) {
     case EPIC_F32: launch_distill<EPIC_F32>(a, forward, blocks, stream); break;

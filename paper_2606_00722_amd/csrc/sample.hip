@@ -49,6 +49,7 @@ struct SampleArgs {
   int32_t* tok;
   float* conf;
   int spread;  // of how many rows those that count are dealt to the first workgroups (0: to their own)
+  int first;   // row of the launch
 };
 
 // floor(mass * part / 2^24) for part <= 2^24
@@ -772,7 +773,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
   constexpr float kSteps = -(float)(LDS::bins / 33);  // steps of a doubling
   const int threads = (int)blockDim.x, waves = threads >> 6;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  int r = (int)blockIdx.x;
+  int r = a.first + (int)blockIdx.x;
   if constexpr (J == 0 || J == 16)
     if (a.spread) r = nth_row(a, s.list, r, wave, waves, (int)threadIdx.x & 63);
   const int b = r / a.rows, i = r - b * a.rows;
@@ -1095,6 +1096,7 @@ struct ProposeArgs {
   float* out_conf;
   int32_t* offsets;
   int B, m, P;
+  int first;  // sequence of the launch
 };
 
 EPIC_DEV bool proposes(int32_t t, float f) { return t >= 0 && f == f; }
@@ -1224,7 +1226,7 @@ template <bool COUNTED>
 __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
   __shared__ uint64_t list[kMaxWaves][64];
   __shared__ int part[kMaxWaves], parts[kMaxWaves];
-  const int b = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
+  const int b = a.first + (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (int)blockDim.x >> 6;
   const int32_t* tok = a.tok + (int64_t)b * a.m;
   const float* conf = a.conf + (int64_t)b * a.m;
@@ -1292,10 +1294,14 @@ __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
 }
 
 template <int DT>
-epic_status launch_sample(const SampleArgs& a, int blocks, hipStream_t stream) {
+epic_status launch_sample(SampleArgs a, int blocks, hipStream_t stream) {
   const int nvec = (a.V + kPer<DT> - 1) / kPer<DT>;
   auto threads = [&](int J) { return std::max(64, ((nvec + J - 1) / J + 63) / 64 * 64); };
-#define EPIC_SAMPLE(J, NT) hipLaunchKernelGGL((sample_kernel<DT, J>), dim3(blocks), dim3(NT), 0, stream, a)
+#define EPIC_SAMPLE(J, NT)                                                                     \
+  launches(blocks, NT, [&](int first, int count) {                                             \
+    a.first = first;                                                                           \
+    hipLaunchKernelGGL((sample_kernel<DT, J>), dim3(count), dim3(NT), 0, stream, a);           \
+  })
   // Eight vectors a lane up to 768 lanes, which two workgroups of a CU can have:
   // 2048 rows of 49152 bfloat16 logits with top-p 0.9 154 us against 204 with
   // sixteen, 2867 of 32768 134 against 171 (46 without filters on either side).
@@ -1331,7 +1337,7 @@ epic_status epic_sample(const epic_rows_desc* logits, const int32_t* d_seqs, int
   if (!d_uniform || !d_tok || !d_conf) return EPIC_ERR_NULL;
   const int es = elem_size(logits->dtype);
   SampleArgs a{(const char*)logits->data, logits->seq_stride * es, logits->row_stride * es, logits->rows, logits->vocab,
-               {d_seqs, d_start, n}, d_uniform, d_temperature, d_top_p, d_min_p, d_top_k, d_tok, d_conf, 0};
+               {d_seqs, d_start, n}, d_uniform, d_temperature, d_top_p, d_min_p, d_top_k, d_tok, d_conf, 0, 0};
   const int blocks = logits->batch * logits->rows;
   if (d_seqs && !d_start && blocks > 256 && blocks <= kSpread) a.spread = blocks;
   switch (logits->dtype) {
@@ -1350,14 +1356,17 @@ epic_status epic_propose(const int32_t* d_tok, const float* d_conf, int32_t batc
   if (!d_offsets) return EPIC_ERR_NULL;
   if (batch > 0 && (!d_cand_seq || !d_cand_pos || !d_cand_tok || !d_cand_conf)) return EPIC_ERR_NULL;
   if (batch > 0 && rows > 0 && (!d_tok || !d_conf)) return EPIC_ERR_NULL;
-  ProposeArgs a{d_tok, d_conf, d_start, d_cand_seq, d_cand_pos, d_cand_tok, d_cand_conf, d_offsets, batch, rows, per_seq};
+  ProposeArgs a{d_tok, d_conf, d_start, d_cand_seq, d_cand_pos, d_cand_tok, d_cand_conf, d_offsets, batch, rows, per_seq, 0};
   const int threads = std::min(1024, std::max(64, (rows + 63) / 64 * 64));
   // in one launch while no wavefront has more than 16 sequences to count
   if (batch > 0 && batch <= 16 * (threads / 64)) {
     hipLaunchKernelGGL(propose_kernel<false>, dim3(batch), dim3(threads), 0, stream, a);
   } else {
     hipLaunchKernelGGL(propose_count_kernel, dim3(1), dim3(1024), 0, stream, a);
-    if (batch > 0) hipLaunchKernelGGL(propose_kernel<true>, dim3(batch), dim3(threads), 0, stream, a);
+    launches(batch, threads, [&](int first, int count) {
+      a.first = first;
+      hipLaunchKernelGGL(propose_kernel<true>, dim3(count), dim3(threads), 0, stream, a);
+    });
   }
   return hipGetLastError() == hipSuccess ? EPIC_OK : EPIC_ERR_HIP;
 }
