@@ -953,8 +953,8 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
   // tokens further than 33 doublings below the largest weigh nothing; -inf is no token
   const float far = M - 33.0f / c;
   const float light = fmaxf(far - fabsf(far) * 1e-5f, kLowest<DT>);
-  auto above = [&](float weighs) {  // a logit below all that weigh as much
-    const float deep = M + (log2f(weighs * (1.f / kOne)) - 0.01f) / c;
+  auto above = [&](float weighs) {  // a logit below all that weigh as much, which 2^31 e does from a half less on
+    const float deep = M + (log2f((weighs - 0.5f) * (1.f / kOne)) - 0.01f) / c;
     return fmaxf(light, deep - fabsf(deep) * 1e-5f - fabsf(M) * 1e-5f);
   };
   uint64_t cut = 0;  // kept: entries not after it

@@ -77,3 +77,26 @@ def test_top_p_close_to_one_at_other_temperatures(epic, dt):
     row = rows_of("flat", 32768, rng)
     check(epic, dt, row / 2, [(0.99999, 0.0), (0.9999, 0.0)], [0.0, 0.5, 1 - 2.0 ** -24], T=0.5)
     check(epic, dt, 2 * row, [(0.99999, 0.0), (0.9999, 0.0)], [0.0, 0.5, 1 - 2.0 ** -24], T=2.0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", SIZES)
+def test_min_p_close_to_zero(epic, dt, V):
+    """From half a unit on: a token passes when its weight rounds up to the
+    least that passes."""
+    rng = np.random.default_rng(V + 1)
+    settings = [(1.0, q) for q in (2.0 ** -32, 2.0 ** -31, 1e-9, 3e-9, 1e-8, 3e-8, 1e-7)]
+    for kind in ("flat", "spread", "few"):
+        check(epic, dt, rows_of(kind, V, rng), settings, [0.0, 1 - 2.0 ** -24])
+
+
+def test_min_p_keeps_the_half_unit(epic):
+    """One token just above, one just below the half unit of every weight."""
+    row = np.full(2000, -60.0, np.float32)
+    row[1999] = 0.0
+    settings = []
+    for i, w in enumerate([1, 2, 3, 5, 9, 17, 40, 70, 100]):
+        edge = math.log((w - 0.5) / 2 ** 31)
+        row[2 * i + 1], row[2 * i] = edge + 2e-5, edge - 2e-5  # x is rounded to within 4e-6
+        settings.append((1.0, w / 2 ** 31))
+    check(epic, "f32", row, settings, [0.0, 2.0 ** -24, 0.5])
