@@ -361,8 +361,9 @@ def _window(seqs, start, B, device):
     i32 = _DTYPES["i32"]
     if seqs is None:
         return 0, 0, 0  # every row counts
-    if seqs.dim() != 2:
-        raise ValueError(f"seqs: int32 [B, n], got {tuple(seqs.shape)}")
+    # a tensor without elements has the address 0, which would say that every row counts
+    if seqs.dim() != 2 or (seqs.shape[1] == 0 and B > 0):
+        raise ValueError(f"seqs: int32 [B, n] with n > 0, got {tuple(seqs.shape)}")
     n = seqs.shape[1]
     return _arg("seqs", seqs, i32, (B, n), device), n, _arg("start", start, i32, (B,), device)
 

@@ -1,5 +1,5 @@
 """The operators on logits rows at the limits of their arguments: more rows
-than one launch can have."""
+than one launch can have, sequences without positions."""
 import numpy as np
 import pytest
 
@@ -71,3 +71,21 @@ def test_proposals_past_one_launch(epic):
     assert off[0] == 0 and torch.equal(off[1:], (tok[:, 0] >= 0).cumsum(0).to(torch.int32))
     assert torch.equal(cand[0][:C], there) and torch.equal(cand[2][:C], there) and (cand[1][:C] == 0).all() and (cand[3][:C] == 0.5).all()
     assert all((c[C:] == -1).all() for c in cand[:3]) and (cand[3][C:] == 0).all()
+
+
+def test_sequences_without_positions_are_refused(epic):
+    """An empty tensor has no address, which is not the same as no sequences."""
+    B, m, V = 2, 3, 64
+    logits = torch.zeros((B, m, V), device=DEV)
+    seqs = torch.zeros((B, 0), dtype=torch.int32, device=DEV)
+    u, tok, conf = torch.zeros((B, m), device=DEV), torch.full((B, m), -7, dtype=torch.int32, device=DEV), torch.zeros((B, m), device=DEV)
+    ids, t = torch.zeros((B, m, 2), dtype=torch.int32, device=DEV), torch.zeros((B, m, 2), device=DEV)
+    loss, stats = torch.full((B, m), 7.0, device=DEV), torch.zeros((B, m, 2), device=DEV)
+    for f in (lambda: epic.sample(logits, seqs, u, tok, conf),
+              lambda: epic.distill_forward(logits, seqs, ids, t, loss, stats),
+              lambda: epic.distill_backward(logits, seqs, ids, t, stats, None, logits)):
+        with pytest.raises(ValueError):
+            f()
+    assert (tok == -7).all() and (loss == 7).all()
+    none = torch.zeros((0, 0), dtype=torch.int32, device=DEV)  # no sequences at all: nothing to do
+    epic.sample(logits[:0], none, u[:0], tok[:0], conf[:0])
