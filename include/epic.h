@@ -416,9 +416,9 @@ epic_status epic_propose(const int32_t* d_tok, const float* d_conf, int32_t batc
  * q = 0.  When every finite logit of the row is listed, q_rest counts as 0.  A
  * row that does not count, whose student logits are all -inf, or that has no
  * entry (without d_teacher_lse: none but -inf) has loss 0 and gradient 0; an id
- * >= vocab gives loss NaN and gradient 0.  NaN and +inf elsewhere give NaN.  z
- * and t / tau are float32: a logit whose quotient is not finite there counts as
- * that infinity.
+ * >= vocab gives loss NaN and gradient 0.  NaN and +inf elsewhere among the
+ * student's logits, the entries' and d_teacher_lse give NaN.  z and t / tau are
+ * float32: a logit whose quotient is not finite there counts as that infinity.
  *
  * d_top_idx int32 and d_top_logit float32 [batch*rows*K], 1 <= K <= 1024, ids
  * in any order; 0 < tau < inf.  d_loss float32 [batch*rows].  d_stats float32

@@ -84,7 +84,8 @@ struct Entries {
 
 // The teacher's shares of the K entries into e.q and what it leaves to the
 // rest, by one wavefront; e.q holds the scaled logits before.  `any`: whether
-// there is an entry to go by.
+// there is an entry to go by.  Of +inf there is no share but NaN, of -inf always
+// none, beside a logsumexp of -inf too.
 EPIC_DEV float teacher_shares(const Entries& e, int K, bool has_lse, float lse, int lane, bool& any) {
   float top = -kInf;
   bool there = false;
@@ -94,7 +95,7 @@ EPIC_DEV float teacher_shares(const Entries& e, int K, bool has_lse, float lse, 
     top = fmaxf(top, e.q[k]);
   }
   any = __ballot(there) != 0;
-  float base = lse;
+  float base = lse < kInf ? lse : __builtin_nanf("");
   if (!has_lse) {
     top = wave_max(top);
     float s = 0.f;
@@ -105,7 +106,7 @@ EPIC_DEV float teacher_shares(const Entries& e, int K, bool has_lse, float lse, 
   float s = 0.f;
   for (int k = lane; k < K; k += 64) {
     if (e.id[k] < 0) continue;
-    const float q = expf(e.q[k] - base);
+    const float t = e.q[k], q = !(t < kInf) ? __builtin_nanf("") : t == -kInf && base == -kInf ? 0.f : expf(t - base);
     e.q[k] = q;
     s += q;
   }
