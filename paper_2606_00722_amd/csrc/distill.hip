@@ -308,6 +308,7 @@ __global__ void __launch_bounds__(1024) distill_forward_kernel(DistillArgs a) {
     }
     kl = wave_sum(kl);
     if (q_rest > 0.f || q_rest != q_rest) kl += q_rest * (logf(q_rest) - lse_rest + lse);
+    if (lse != lse) kl = lse;  // also where the teacher has no share to multiply it with
     if (lane == 0) {
       const bool dead = !any || empty;
       a.loss[r] = dead ? 0.f : kl * a.tau * a.tau;

@@ -1,5 +1,5 @@
 """epic_distill_forward and epic_distill_backward where the teacher's numbers
-are infinite."""
+are infinite or the student's are none."""
 import math
 
 import numpy as np
@@ -72,3 +72,11 @@ def test_teacher_of_nothing_but_masks(epic):
     assert abs(loss[0, 0] - want) <= 1e-5  # 6 roundings of numbers up to 10
     for g in grads:
         assert np.abs(g[0, 0] - grad).max() <= 1e-5
+
+
+def test_nan_of_the_student_beside_no_share(epic):
+    """Every token listed, none with a share: the row's NaN is still seen."""
+    l = np.zeros((1, 1, 3))
+    l[0, 0, 1] = math.nan
+    loss, grads = run(epic, l, np.array([[[0, 1, 2]]]), np.full((1, 1, 3), -math.inf), np.zeros((1, 1)))
+    assert np.isnan(loss).all() and all(np.isnan(g).all() for g in grads)
