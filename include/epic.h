@@ -421,7 +421,8 @@ epic_status epic_propose(const int32_t* d_tok, const float* d_conf, int32_t batc
  * float32: a logit whose quotient is not finite there counts as that infinity.
  *
  * d_top_idx int32 and d_top_logit float32 [batch*rows*K], 1 <= K <= 1024, ids
- * in any order; 0 < tau < inf.  d_loss float32 [batch*rows].  d_stats float32
+ * in any order; 0 < tau < inf with log2(e) / tau finite in float32 (tau > 4.24e-39),
+ * else EPIC_ERR_ARG.  d_loss float32 [batch*rows].  d_stats float32
  * [batch*rows*2] receives lse and lse_rest of each row for the backward pass.
  * Gradients: grad (its data, of the logits' type and shape, strides of its
  * own, rounded to nearest even from float32) receives weight[row] times the

@@ -483,7 +483,7 @@ epic_status distill(const epic_rows_desc* logits, const int32_t* d_seqs, int32_t
                     hipStream_t stream) {
   epic_status st = check_rows(logits, d_seqs, n);
   if (st != EPIC_OK) return st;
-  if (K < 1 || K > 1024 || !(tau > 0.f) || !(tau < kInf) || !(1.f / tau < kInf)) return EPIC_ERR_ARG;
+  if (K < 1 || K > 1024 || !(tau > 0.f) || !(tau < kInf) || !(kLog2e / tau < kInf)) return EPIC_ERR_ARG;
   if (!forward && !grad) return EPIC_ERR_NULL;
   if (grad) {
     if ((st = check_rows(grad, nullptr, 0)) != EPIC_OK) return st;

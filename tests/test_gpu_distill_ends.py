@@ -1,5 +1,5 @@
 """epic_distill_forward and epic_distill_backward where the teacher's numbers
-are infinite or the student's are none."""
+are infinite or the student's are none, and at the least tau."""
 import math
 
 import numpy as np
@@ -80,3 +80,17 @@ def test_nan_of_the_student_beside_no_share(epic):
     l[0, 0, 1] = math.nan
     loss, grads = run(epic, l, np.array([[[0, 1, 2]]]), np.full((1, 1, 3), -math.inf), np.zeros((1, 1)))
     assert np.isnan(loss).all() and all(np.isnan(g).all() for g in grads)
+
+
+def test_tiny_tau(epic):
+    """A tau whose log2(e) / tau is past float32 is refused; one a little above
+    leaves the largest logit all of the mass."""
+    V, K = 50, 2
+    l, ids, t = np.zeros((1, 1, V)), np.array([[[7, -1]]]), np.zeros((1, 1, K))
+    for tau in (1e-44, 3e-39, 4.2e-39):
+        with pytest.raises(epic.EpicError) as e:
+            run(epic, l, ids, t, None, tau)
+        assert e.value.code == -2
+    l[0, 0, 7] = 1.0
+    loss, grads = run(epic, l, ids, t, None, 4.3e-39)
+    assert loss[0, 0] == 0 and all((g == 0).all() for g in grads)
