@@ -1120,11 +1120,11 @@ EPIC_DEV uint64_t merge64(uint64_t a, uint64_t b) {
 }
 
 // Adds the rows with a token among 64 H rows from `at` of eight sequences first,
-// first + step, ..., whose loads are all in flight together; counts end at P.
-// True while a sequence has less.
+// first + step, ..., whose loads are all in flight together, to n of lane 0, 1,
+// ...; counts end at P.
 constexpr int kCounts = 8;
 template <int H>
-EPIC_DEV bool count_round(const ProposeArgs& a, int first, int step, int64_t at, int lane, int (&n)[kCounts]) {
+EPIC_DEV void count_round(const ProposeArgs& a, int first, int step, int at, int lane, int& n) {
   int32_t t[kCounts][H];
   float f[kCounts][H];
 #pragma unroll
@@ -1132,63 +1132,72 @@ EPIC_DEV bool count_round(const ProposeArgs& a, int first, int step, int64_t at,
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       // never a branch around a load: they would wait for each other
-      const int64_t i = at + h * 64 + lane;
-      const int64_t from = (int64_t)min(first + g * step, a.B - 1) * a.m + (i < a.m ? i : a.m - 1);
-      t[g][h] = a.tok[from];
-      f[g][h] = a.conf[from];
+      const int64_t row = (int64_t)min(first + g * step, a.B - 1) * a.m;
+      const uint32_t i = (uint32_t)min(at + h * 64 + lane, a.m - 1);
+      t[g][h] = (a.tok + row)[i];
+      f[g][h] = (a.conf + row)[i];
     }
-  bool open = false;
 #pragma unroll
   for (int g = 0; g < kCounts; ++g) {
+    int c = 0;
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const bool there = at + h * 64 + lane < a.m && first + g * step < a.B;
-      n[g] += __popcll((unsigned long long)__ballot(there && proposes(t[g][h], f[g][h])));
-    }
-    n[g] = min(n[g], a.P);
-    open = open || (n[g] < a.P && first + g * step < a.B);
+    for (int h = 0; h < H; ++h)
+      c += __popcll((unsigned long long)__ballot(at + h * 64 + lane < a.m && proposes(t[g][h], f[g][h])));
+    n += lane == g ? c : 0;
   }
-  return open;
+  n = min(n, a.P);
 }
-// min(P, rows of sequence b with a token), by one wavefront, 512 rows at a time
-EPIC_DEV int count_rows(const ProposeArgs& a, int b, int lane) {
-  constexpr int G = 8;
+// n and the rows with a token of sequence b from row `at` on, at most P, by one
+// wavefront, 64 G rows at a time
+template <int G>
+EPIC_DEV int count_rows(const ProposeArgs& a, int b, int at, int lane, int n) {
   const int32_t* tok = a.tok + (int64_t)b * a.m;
   const float* conf = a.conf + (int64_t)b * a.m;
-  int n = 0;
 #pragma unroll 1
-  for (int64_t at = lane; at - lane < a.m && n < a.P; at += 64 * G) {
+  for (at += lane; at - lane < a.m && n < a.P; at += 64 * G) {
     int32_t t[G];
     float f[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      t[g] = -1;
-      f[g] = 0.f;
-      if (at + g * 64 < a.m) {
-        t[g] = tok[at + g * 64];
-        f[g] = conf[at + g * 64];
-      }
+      const uint32_t i = (uint32_t)min(at + g * 64, a.m - 1);
+      t[g] = tok[i];
+      f[g] = conf[i];
     }
 #pragma unroll
-    for (int g = 0; g < G; ++g) n += __popcll((unsigned long long)__ballot(proposes(t[g], f[g])));
+    for (int g = 0; g < G; ++g) n += __popcll((unsigned long long)__ballot(at + g * 64 < a.m && proposes(t[g], f[g])));
   }
   return min(n, a.P);
 }
-// min(P, rows with a token) of eight sequences, by one wavefront.  Most are settled
-// by their first 64 rows.  Up to 320 rows the others' rest follows at once (64
-// sequences of 300 rows that have fewer than P: 10 us a call against 13 for one
-// sequence after another), longer ones go one by one (64 of 1024: 13 us against 20).
-EPIC_DEV void count_eight(const ProposeArgs& a, int first, int step, int lane, int (&n)[kCounts]) {
-#pragma unroll
-  for (int g = 0; g < kCounts; ++g) n[g] = 0;
-  if (a.m <= 0 || !count_round<1>(a, first, step, 0, lane, n) || a.m <= 64) return;
-  if (a.m <= 64 + 256) {
-    count_round<4>(a, first, step, 64, lane, n);
-    return;
+// min(P, rows with a token) of eight sequences first, first + step, ..., in lanes
+// 0, 1, ... (0 past the last sequence and in the other lanes), by one wavefront.
+// Most are settled by their first 64 rows.  Up to 320 rows the rest of more than
+// two follows at once (64 sequences of 300 rows that have fewer than P: 8.9 us a
+// call on the GPU), else one sequence after another (64 of 1024: 14.1 us; 4 of 130:
+// 5.3, at once 5.9).  Counts stay in a register of one lane each: eight in every
+// lane, and the loads beside them, took more registers than there are.  Batches
+// counted by a launch of their own take 5.5 to 12.5 us (17 to 1024 sequences of up
+// to 64 rows).
+EPIC_DEV int count_eight(const ProposeArgs& a, int first, int step, int lane) {
+  int n = 0;
+  if (a.m <= 0 || first >= a.B) return n;
+  const bool there = lane < kCounts && first + lane * step < a.B;
+  count_round<1>(a, first, step, 0, lane, n);
+  if (a.m > 64) {
+    uint64_t open = __ballot(there && n < a.P);
+    const bool few = a.m <= 64 + 256;
+    if (few && __popcll((unsigned long long)open) > 2) {
+      count_round<4>(a, first, step, 64, lane, n);
+    } else {
+      while (open) {
+        const int g = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)open) - 1), b = first + g * step;
+        open &= open - 1;
+        const int so_far = __builtin_amdgcn_readlane(n, g);
+        const int c = few ? count_rows<4>(a, b, 64, lane, so_far) : count_rows<16>(a, b, 64, lane, so_far);
+        n = lane == g ? c : n;
+      }
+    }
   }
-#pragma unroll
-  for (int g = 0; g < kCounts; ++g)
-    if (n[g] < a.P && first + g * step < a.B) n[g] = count_rows(a, first + g * step, lane);
+  return there ? n : 0;
 }
 
 // the offsets of a large batch: one workgroup, sequences dealt to wavefronts
@@ -1200,11 +1209,8 @@ __global__ void __launch_bounds__(1024) propose_count_kernel(ProposeArgs a) {
   for (int b0 = 0; b0 < a.B; b0 += 1024) {
 #pragma unroll 1
     for (int k = wave * kCounts; k < 1024; k += 16 * kCounts) {
-      int c[kCounts];
-      count_eight(a, b0 + k, 1, lane, c);
-#pragma unroll
-      for (int g = 0; g < kCounts; ++g)
-        if (lane == g) n[k + g] = c[g];
+      const int c = count_eight(a, b0 + k, 1, lane);
+      if (lane < kCounts) n[k + lane] = c;
     }
     __syncthreads();
     if (wave == 0) {
@@ -1241,14 +1247,12 @@ __global__ void __launch_bounds__(1024) propose_kernel(ProposeArgs a) {
     int before = 0, all = 0;
 #pragma unroll 1
     for (int o = wave; o < a.B; o += waves * kCounts) {
-      int c[kCounts];
-      count_eight(a, o, waves, lane, c);
-#pragma unroll
-      for (int g = 0; g < kCounts; ++g) {
-        before += o + g * waves < b ? c[g] : 0;
-        all += c[g];
-      }
+      const int c = count_eight(a, o, waves, lane);
+      before += o + lane * waves < b ? c : 0;
+      all += c;
     }
+    before = (int)wave_sum64((uint64_t)before);
+    all = (int)wave_sum64((uint64_t)all);
     if (lane == 0) {
       part[wave] = before;
       parts[wave] = all;
