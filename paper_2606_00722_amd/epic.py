@@ -328,8 +328,8 @@ def _dtypes() -> dict:
 
         lib()
         _torch = torch
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
-        _DTYPES.update(i32=torch.int32, f32=torch.float32)
+        # at once: other threads go by whether it is empty
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, "i32": torch.int32, "f32": torch.float32})
     return _DTYPES
 
 
