@@ -355,9 +355,12 @@ typedef struct {
  * numbers: one token and its confidence for every row that counts.
  *
  * With M the row's largest logit and T its temperature, token t has
- *   x_t = (l_t - M) * c,  c = log2(e) / T rounded to float32,  e_t = 2^x_t,
- *   w_t = floor(2^31 * e_t + 1/2),  a whole number; W = sum of all w_t
- * (x, e and the sum with 1/2 in float32).  Sums of whole numbers depend on no order, so neither does the token drawn.
+ *   x_t = (l_t - M) * c,  c = log2(e) / T rounded to float32, at most 1e30,
+ *   e_t = 2^x_t,  w_t = floor(2^31 * e_t + 1/2),  a whole number; W = sum of all
+ *   w_t
+ * (x, e and the sum with 1/2 in float32).  Sums of whole numbers depend on no
+ * order, so neither does the token drawn.  A weight is off by up to half a unit:
+ * tokens below 2^-32 of the likeliest one's probability are never drawn.
  * NaN and -inf logits have w = 0 and are never drawn.
  * Tokens are ordered by descending logit, ties to the lower id.  Kept are the
  * tokens that pass all of
@@ -419,6 +422,7 @@ epic_status epic_propose(const int32_t* d_tok, const float* d_conf, int32_t batc
  * >= vocab gives loss NaN and gradient 0.  NaN and +inf elsewhere among the
  * student's logits, the entries' and d_teacher_lse give NaN.  z and t / tau are
  * float32: a logit whose quotient is not finite there counts as that infinity.
+ * Exponentials below 2^-126 may count as 0.
  *
  * d_top_idx int32 and d_top_logit float32 [batch*rows*K], 1 <= K <= 1024, ids
  * in any order; 0 < tau < inf with log2(e) / tau finite in float32 (tau > 4.24e-39),

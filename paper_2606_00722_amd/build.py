@@ -19,13 +19,14 @@ SOURCES = ([os.path.join(CSRC, "epic.hip"), os.path.join(CSRC, "tables.cpp")]
            + [os.path.join(CSRC, f"epic_w{w}.hip") for w in WIDTHS]
            + [os.path.join(CSRC, "sample.hip"), os.path.join(CSRC, "distill.hip")])
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
+         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # Without machine LICM the walk kernels need 100 to 220 vector registers a lane
 # instead of 225 to 256 (it hoists LDS addresses and other cheap constants out
 # of the whole walk), so the 1024-thread kernels of 16-word item sets spill 120
 # to 270 bytes a lane instead of 310 to 460: C-like 16 x 256 selection 11.7 ->
-# 10.2 ms, validation 7.3 -> 6.8; the 512-thread kernels are within 2 %.
-FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
-         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# 10.2 ms, validation 7.3 -> 6.8; the 512-thread kernels are within 2 %.  The
+# operators on logits rows are built with it.
 WALK_FLAGS = ["-mllvm", "-disable-machine-licm"]
 NO_WALKS = ("sample.hip", "distill.hip")
 

@@ -139,19 +139,18 @@ struct Row {
   }
 };
 
-// BINS: of the histogram, ROOM: of the list, the tokens that are put in order in
-// LDS.  A step in which a border lies should hold no more than ROOM tokens: 33
-// doublings of weight in 1024 steps put 90 of 32768 normally distributed logits
-// (deviation 2) in one, so longer rows have more steps.  That does not part
-// equal logits, of which 131072 in bfloat16 have hundreds of a value: rows that
-// take a CU for themselves have a longer list.
-template <int BINS, int ROOM>
+// BINS: of the histogram; room: of the list, the tokens that are put in order in
+// LDS.  A step in which a border lies should hold no more than that: 33 doublings
+// of weight in 1024 steps put 90 of 32768 normally distributed logits (deviation
+// 2) in one, so longer rows have more steps.  That does not part equal logits, of
+// which 131072 in bfloat16 have hundreds of a value: such rows go another way.
+template <int BINS>
 struct SampleLds {
-  static constexpr int bins = BINS, room = ROOM;
+  static constexpr int bins = BINS, room = 512;
   static constexpr int skew = BINS + BINS / 16;  // 17 words of 8 bytes every 16 bins
   uint64_t hist[skew];
-  uint64_t list[ROOM];  // entries, in no order
-  uint32_t weights[ROOM];
+  uint64_t list[room];  // entries, in no order
+  uint32_t weights[room];
   uint64_t mass[kMaxWaves];
   float top[kMaxWaves];
   int listed;
@@ -767,7 +766,7 @@ EPIC_DEV int nth_row(const SampleArgs& a, uint64_t* masks, int x, int wave, int 
 
 template <int DT, int J>
 __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
-  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024, 512>;
+  using LDS = SampleLds<J == 0 || J == 16 ? 4096 : J == 8 ? 2048 : 1024>;
   __shared__ LDS s;
   constexpr int E = kPer<DT>;
   constexpr float kSteps = -(float)(LDS::bins / 33);  // steps of a doubling
