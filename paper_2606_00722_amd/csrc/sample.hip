@@ -1084,8 +1084,8 @@ __global__ void __launch_bounds__(1024) sample_kernel(SampleArgs a) {
 // every workgroup counts them itself, which is one load of 64 tokens for most
 // sequences; a batch too large for that has them counted by a launch before.
 //
-// Bound by latency: 64 sequences of 1024 positions take 7.7 us on the GPU (0.5 MB,
-// 0.1 us of reading), 8 of 128 take 4.8; the sort of 64 is 21 exchanges, a merge
+// Bound by latency: 64 sequences of 1024 positions take 7.8 us on the GPU (0.5 MB,
+// 0.1 us of reading), 8 of 128 take 4.9; the sort of 64 is 21 exchanges, a merge
 // six, and each load of the counting is one trip to memory.
 struct ProposeArgs {
   const int32_t* tok;
