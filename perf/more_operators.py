@@ -127,8 +127,9 @@ def _quantized(x):
     x = x.float()
     top = x.abs().amax(-1, keepdim=True)
     some = top > 0
-    q = torch.round(x * torch.where(some, 127.0 / torch.where(some, top, 1.0), 0.0))
-    return q, (top / 127.0)[..., 0]
+    # tensors on both sides: of a number over a tensor, torch takes the reciprocal
+    ratio = torch.where(some, torch.full_like(top, 127.0) / torch.where(some, top, 1.0), 0.0)
+    return torch.round(x * ratio), (top / torch.full_like(top, 127.0))[..., 0]
 
 
 def prepare(case, seed):
@@ -328,7 +329,7 @@ def _exact_logits(case, s):
         at = counted[b].nonzero()[:, 0]
         x = s["hidden"][b, at].float()
         top = x.abs().amax(-1, keepdim=True)
-        q = torch.round((x * (127.0 / top)).double())
+        q = torch.round((x * (torch.full_like(top, 127.0) / top)).double())
         out[b, at] = torch.mm(q * (top.double() / 127.0), q_head.t())
     return {"logits": out}
 
