@@ -446,6 +446,83 @@ epic_status epic_distill_backward(const epic_rows_desc* logits, const int32_t* d
                                   int32_t K, const float* d_teacher_lse, float tau, const float* d_stats,
                                   const float* d_weight, const epic_rows_desc* grad, hipStream_t stream);
 
+/* ---- Between hidden states and logits: the head -------------------------
+ *
+ * A denoiser's last step is a product with its head, a matrix W of one row of
+ * `width` numbers per token.  The operators below compute what the rows that
+ * count (as above; hidden states are rows whose `vocab` is the width) need of
+ * it: their logits from a head in 8 bits, and the cross entropy of their tokens
+ * with its gradient, for which no logits are kept.  Rows that do not count cost
+ * next to nothing: the others are moved together first.
+ *
+ * 1 <= width <= 65536 and batch * rows <= 2^24, else EPIC_ERR_UNSUPPORTED.
+ * Workspaces are device memory of the caller's, 256-byte aligned, of the bytes
+ * that the call's *_workspace_bytes gives for the same descriptors (0 where the
+ * call would refuse them); what they hold before does not matter and nothing is
+ * kept in them.  Calls that can overlap need one each.  The calls allocate
+ * nothing and may be captured in a HIP graph; the same call on the same inputs
+ * gives the same bits (the order of the sums goes by the sizes of the call).
+ *
+ * epic_quantize_rows: rows of numbers to 8 bits, each with a scale of its own.
+ *   a = max |x|, scale = a / 127, q = x * (127 / a) rounded to the nearest
+ *   whole number, ties to the even one (both quotients and the product rounded
+ *   to float32).  A row with a below 1e-30 has scale 0 and q 0; a row with a NaN
+ *   or an infinity has scale NaN and q 0.
+ * Row (b, i) goes to q[(b*rows + i)*q_stride ..], zeros behind its `vocab`
+ * numbers; q is 16-byte aligned, q_stride a multiple of 128 and at least `vocab`
+ * (the head of epic_logits_q8 needs the least such).  d_scale float32
+ * [batch*rows].  A head is quantised once, as batch = 1 and a row per token.
+ *
+ * epic_logits_q8: logits of the rows that count,
+ *   l_j = (sum_k q_k q_jk) * scale * scale_j
+ * with q and scale of the row of hidden states quantised as above, in the call,
+ * and q_j and scale_j the head's.  The sum is exact; it is rounded to float32,
+ * as are the two products, and the logit to its type.  logits: rows of `vocab`
+ * tokens, of any of the types, beside the hidden states' (same batch and rows);
+ * the rows must not overlap, and those that do not count are left as they are. */
+epic_status epic_quantize_rows(const epic_rows_desc* x, int8_t* d_q, int64_t q_stride, float* d_scale,
+                               hipStream_t stream);
+size_t epic_logits_q8_workspace_bytes(const epic_rows_desc* hidden);
+epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, int32_t n, const int32_t* d_start,
+                           const int8_t* d_q, int64_t q_stride, const float* d_q_scale, const epic_rows_desc* logits,
+                           void* d_workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Cross entropy of the rows' tokens over the whole vocabulary, from hidden
+ * states h and head W (batch 1, a row per token, of the hidden states' type):
+ *   l_j = sum_k h_k W_jk,  lse = log sum_j exp(l_j),  loss = lse - l_y,
+ * and, with G_ij = weight_i (exp(l_ij - lse_i) - [j = y_i]), the gradients of
+ * sum_i weight_i loss_i:  dh_i = sum_j G_ij W_j,  dW_j = sum_i G_ij h_i.
+ * A row counts when its position is masked and its token d_target (int32
+ * [batch*rows]) is at least 0.  Rows that do not count have loss 0, lse 0 and
+ * gradient 0; their hidden states are not read.  A token >= the vocabulary gives
+ * loss NaN, and the row adds nothing to the gradients.  NaN and infinities go
+ * their way through the sums; an infinite logit gives NaN.
+ *
+ * The gradients go by pieces of the vocabulary: a piece's logits are computed
+ * again from the forward pass's lse, G is kept for one piece, and two products
+ * read it.  Sums are float32.  16-bit inputs are multiplied as they are, and G
+ * is rounded to their type; of float32 inputs and their G the products take 22
+ * bits and a sign, relative to numbers of at least 2^-17 of the tensor's largest
+ * (smaller ones: 2^-40 of it).  float16 G is scaled so that exp(l - lse) from
+ * 2^-24 on is a normal number, whatever the weight.
+ *
+ * d_loss and d_lse float32 [batch*rows].  d_weight float32 [batch*rows]: the
+ * upstream gradient of each row's loss (NULL: 1).  grad_hidden (shape and type
+ * of the hidden states, strides of its own) may be the hidden states themselves
+ * (the same data and strides); grad_head (shape and type of the head) may not
+ * overlap other arguments.  Either may be NULL, then it is not computed.  Both
+ * are written, not added to. */
+size_t epic_head_loss_workspace_bytes(const epic_rows_desc* hidden, const epic_rows_desc* head, int32_t backward);
+epic_status epic_head_loss_forward(const epic_rows_desc* hidden, const int32_t* d_seqs, int32_t n,
+                                   const int32_t* d_start, const epic_rows_desc* head, const int32_t* d_target,
+                                   float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+epic_status epic_head_loss_backward(const epic_rows_desc* hidden, const int32_t* d_seqs, int32_t n,
+                                    const int32_t* d_start, const epic_rows_desc* head, const int32_t* d_target,
+                                    const float* d_lse, const float* d_weight, const epic_rows_desc* grad_hidden,
+                                    const epic_rows_desc* grad_head, void* d_workspace, size_t workspace_bytes,
+                                    hipStream_t stream);
+
 const char* epic_status_string(epic_status s);
 
 #ifdef __cplusplus

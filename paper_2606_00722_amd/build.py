@@ -3,7 +3,8 @@
 The kernels of each item width are a compilation unit of their own
 (csrc/epic_w<W>.hip); the units compile in parallel, then link with the C ABI
 unit (csrc/epic.hip), the host tables (csrc/tables.cpp) and the operators on
-logits rows (csrc/sample.hip, csrc/distill.hip)."""
+logits rows and the head before them (csrc/sample.hip, csrc/distill.hip,
+csrc/head.hip)."""
 from __future__ import annotations
 
 import os
@@ -17,7 +18,7 @@ LIB = os.path.join(HERE, "libepic.so")
 WIDTHS = (1, 2, 4, 8, 16)
 SOURCES = ([os.path.join(CSRC, "epic.hip"), os.path.join(CSRC, "tables.cpp")]
            + [os.path.join(CSRC, f"epic_w{w}.hip") for w in WIDTHS]
-           + [os.path.join(CSRC, "sample.hip"), os.path.join(CSRC, "distill.hip")])
+           + [os.path.join(CSRC, "sample.hip"), os.path.join(CSRC, "distill.hip"), os.path.join(CSRC, "head.hip")])
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -28,7 +29,7 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
 # 10.2 ms, validation 7.3 -> 6.8; the 512-thread kernels are within 2 %.  The
 # operators on logits rows are built with it.
 WALK_FLAGS = ["-mllvm", "-disable-machine-licm"]
-NO_WALKS = ("sample.hip", "distill.hip")
+NO_WALKS = ("sample.hip", "distill.hip", "head.hip")
 
 
 def build_library() -> str:

@@ -30,6 +30,8 @@ FUNCTIONS = ["epic_ctx_create", "epic_ctx_destroy", "epic_workspace_bytes", "epi
              "epic_ctx_set_witness_lds", "epic_ctx_kernel_stats",
              "epic_witness_workspace_bytes", "epic_witness",
              "epic_sample", "epic_propose", "epic_distill_forward", "epic_distill_backward",
+             "epic_quantize_rows", "epic_logits_q8_workspace_bytes", "epic_logits_q8",
+             "epic_head_loss_workspace_bytes", "epic_head_loss_forward", "epic_head_loss_backward",
              "epic_diag_lds_stream", "epic_diag_clock_rates", "epic_status_string"]
 KERNEL_KINDS = ["lexmemo", "base", "validate", "select", "fallback", "spec_bookkeeping", "spec_unused"]
 
@@ -115,6 +117,19 @@ def lib() -> ctypes.CDLL:
         L.epic_distill_forward.restype = ctypes.c_int
         L.epic_distill_backward.argtypes = [rows, P, i32, P, P, P, i32, P, f32, P, P, rows, P]
         L.epic_distill_backward.restype = ctypes.c_int
+        i64 = ctypes.c_int64
+        L.epic_quantize_rows.argtypes = [rows, P, i64, P, P]
+        L.epic_quantize_rows.restype = ctypes.c_int
+        L.epic_logits_q8_workspace_bytes.argtypes = [rows]
+        L.epic_logits_q8_workspace_bytes.restype = sz
+        L.epic_logits_q8.argtypes = [rows, P, i32, P, P, i64, P, rows, P, sz, P]
+        L.epic_logits_q8.restype = ctypes.c_int
+        L.epic_head_loss_workspace_bytes.argtypes = [rows, rows, i32]
+        L.epic_head_loss_workspace_bytes.restype = sz
+        L.epic_head_loss_forward.argtypes = [rows, P, i32, P, rows, P, P, P, P, sz, P]
+        L.epic_head_loss_forward.restype = ctypes.c_int
+        L.epic_head_loss_backward.argtypes = [rows, P, i32, P, rows, P, P, P, rows, rows, P, sz, P]
+        L.epic_head_loss_backward.restype = ctypes.c_int
         L.epic_diag_lds_stream.argtypes = [i32, i32, i32, P, P]
         L.epic_diag_lds_stream.restype = ctypes.c_int
         L.epic_diag_clock_rates.argtypes = [ctypes.POINTER(i32), ctypes.POINTER(i32)]
@@ -460,3 +475,115 @@ def distill_backward(logits, seqs, top_idx, top_logit, stats, weight, grad, star
     _call("epic_distill_backward", dev, stream, ctypes.byref(rows), sp, n, st, ti, tl, K, te, tau,
           _arg("stats", stats, f32, (B, m, 2), dev), _arg("weight", weight, f32, (B, m), dev),
           ctypes.byref(_rows("grad", grad, dev)))
+
+
+# ---------------------------------------------------------------------------
+# Between hidden states and logits: the head.  Hidden states are a tensor
+# [B, m, d] like logits are one of [B, m, V], a head one of [V, d].  Workspaces
+# are uint8 tensors of the caller's, from the alloc_*_workspace of the call for
+# tensors of the same shapes, types and strides; calls that can overlap (on other
+# streams, in graphs) need one each.
+
+
+def _matrix(name, t, device=None) -> _Rows:
+    if t.dim() != 2:
+        raise ValueError(f"{name}: a [V, d] tensor, got {tuple(t.shape)}")
+    return _rows(name, t.unsqueeze(0), device)
+
+
+def _scratch(workspace, device):
+    """Address and bytes of the aligned part of a workspace."""
+    if workspace is None or workspace.dtype is not _torch.uint8 or workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous uint8 on cuda:{device}")
+    p = workspace.data_ptr()
+    at = (p + 255) & ~255
+    return at, max(0, workspace.numel() - (at - p))
+
+
+def q8_width(d: int) -> int:
+    """Bytes of a row of a head in 8 bits: its width up to a multiple of 128."""
+    return (d + 127) // 128 * 128
+
+
+def alloc_q8(V: int, d: int, device="cuda"):
+    """What quantize writes: numbers int8 [V, q8_width(d)], scales float32 [V]."""
+    import torch
+
+    return torch.empty((V, q8_width(d)), dtype=torch.int8, device=device), torch.empty(V, dtype=torch.float32, device=device)
+
+
+def quantize(x, q, scale, stream=None):
+    """epic_quantize_rows of a matrix [V, d] (float32, float16 or bfloat16) into
+    q int8 [V, w] with w a multiple of 128, and scale float32 [V]."""
+    rows = _matrix("x", x)
+    dev, (V, d) = x.get_device(), x.shape
+    if q.dim() != 2:
+        raise ValueError(f"q: int8 [V, w], got {tuple(q.shape)}")
+    w = q.shape[1]
+    _call("epic_quantize_rows", dev, stream, ctypes.byref(rows), _arg("q", q, _torch.int8, (V, w), dev), w,
+          _arg("scale", scale, _DTYPES["f32"], (V,), dev))
+
+
+def alloc_logits_q8_workspace(hidden):
+    """Device memory for logits_q8 of hidden states like these."""
+    rows = _rows("hidden", hidden)
+    return _torch.empty(int(_lib.epic_logits_q8_workspace_bytes(ctypes.byref(rows))) + 256, dtype=_torch.uint8, device=hidden.device)
+
+
+def logits_q8(hidden, seqs, q, scale, logits, workspace, start=None, stream=None):
+    """epic_logits_q8: of the rows of hidden [B, m, d] that count (seqs, start as
+    in sample) the logits [B, m, V], from a head that quantize wrote: q int8
+    [V, q8_width(d)], scale float32 [V].  Other rows of logits stay as they are."""
+    rows = _rows("hidden", hidden)
+    dev, (B, m, d) = hidden.get_device(), hidden.shape
+    out = _rows("logits", logits, dev)
+    V, w = logits.shape[2], q8_width(d)
+    sp, n, st = _window(seqs, start, B, dev)
+    if q is None or scale is None:
+        raise ValueError("q and scale are needed")
+    wp, wb = _scratch(workspace, dev)
+    _call("epic_logits_q8", dev, stream, ctypes.byref(rows), sp, n, st, _arg("q", q, _torch.int8, (V, w), dev), w,
+          _arg("scale", scale, _DTYPES["f32"], (V,), dev), ctypes.byref(out), wp, wb)
+
+
+def alloc_head_loss_workspace(hidden, head, backward=True):
+    """Device memory for head_loss_forward (and _backward) of tensors like these."""
+    rows, mat = _rows("hidden", hidden), _matrix("head", head, hidden.get_device())
+    n = int(_lib.epic_head_loss_workspace_bytes(ctypes.byref(rows), ctypes.byref(mat), int(bool(backward))))
+    return _torch.empty(n + 256, dtype=_torch.uint8, device=hidden.device)
+
+
+def head_loss_forward(hidden, seqs, head, target, loss, lse, workspace, start=None, stream=None):
+    """epic_head_loss_forward: cross entropy of the tokens target int32 [B, m]
+    (below 0: the row does not count) in the rows of hidden [B, m, d] whose
+    positions are masked, over the tokens of head [V, d]: loss and lse float32
+    [B, m] are written."""
+    rows = _rows("hidden", hidden)
+    dev, (B, m, _) = hidden.get_device(), hidden.shape
+    f32 = _DTYPES["f32"]
+    sp, n, st = _window(seqs, start, B, dev)
+    if target is None or loss is None or lse is None:
+        raise ValueError("target, loss and lse are needed")
+    wp, wb = _scratch(workspace, dev)
+    _call("epic_head_loss_forward", dev, stream, ctypes.byref(rows), sp, n, st, ctypes.byref(_matrix("head", head, dev)),
+          _arg("target", target, _DTYPES["i32"], (B, m), dev), _arg("loss", loss, f32, (B, m), dev),
+          _arg("lse", lse, f32, (B, m), dev), wp, wb)
+
+
+def head_loss_backward(hidden, seqs, head, target, lse, weight, grad_hidden, grad_head, workspace, start=None, stream=None):
+    """epic_head_loss_backward: the gradients of sum(weight * loss) with the lse
+    of a head_loss_forward over the same inputs, weight float32 [B, m] or None
+    for 1: grad_hidden (like hidden, or hidden itself) and grad_head (like head);
+    either may be None."""
+    rows = _rows("hidden", hidden)
+    dev, (B, m, _) = hidden.get_device(), hidden.shape
+    f32 = _DTYPES["f32"]
+    sp, n, st = _window(seqs, start, B, dev)
+    if target is None or lse is None:
+        raise ValueError("target and lse are needed")
+    wp, wb = _scratch(workspace, dev)
+    gh = None if grad_hidden is None else ctypes.byref(_rows("grad_hidden", grad_hidden, dev))
+    gw = None if grad_head is None else ctypes.byref(_matrix("grad_head", grad_head, dev))
+    _call("epic_head_loss_backward", dev, stream, ctypes.byref(rows), sp, n, st, ctypes.byref(_matrix("head", head, dev)),
+          _arg("target", target, _DTYPES["i32"], (B, m), dev), _arg("lse", lse, f32, (B, m), dev),
+          _arg("weight", weight, f32, (B, m), dev), gh, gw, wp, wb)
