@@ -4,6 +4,22 @@
 
 namespace epic_rows {
 
+// How numbers are multiplied.  float32 goes one of two ways: as it is, at a
+// sixteenth of the rate of 16-bit numbers, or as the sum of two float16 numbers,
+// three products of which keep 22 bits and a sign, at a third of it, for which
+// hidden states and head have to be written out so first.
+enum Form { kFormBf16, kFormF16, kFormF32, kFormSplit };
+template <int FORM>
+constexpr int kDtype = FORM == kFormBf16 ? EPIC_BF16 : FORM == kFormF16 ? EPIC_F16 : EPIC_F32;
+template <int FORM>
+constexpr int kKind = FORM == kFormBf16 ? kBf16 : FORM == kFormF32 ? kF32 : kF16;
+template <int FORM>
+constexpr int kPairs = FORM == kFormSplit ? 3 : 1;
+template <int FORM>
+constexpr int kPacked = FORM == kFormF32 ? 4 : 2;  // bytes of a number that products read
+template <int FORM>
+constexpr bool kScaled = FORM == kFormF16 || FORM == kFormSplit;  // numbers are brought into float16's range
+
 // ------------------------------------------------------- rows that count
 // Which rows of the window count, and what is kept of each, one after another
 // (the count-th and later entries are not written): `src` the row's number.
@@ -32,10 +48,12 @@ struct GatherArgs {
   char* out;         // packed rows
   char* out2;        // 16-bit numbers with the rows' powers of two, for the product over rows
   int64_t stride, plane;  // bytes
+  int width;         // of packed rows, in numbers
   float* scale;      // 8 bits: the rows' scales
   const float* tops; // 32 bits: largest magnitudes of hidden states and head, in parts
   int top_parts[2];
   int per;           // rows of a workgroup
+  int2* counts;      // of every 64 rows, or NULL
   int V;
 };
 
@@ -43,7 +61,10 @@ constexpr int kGather = 256;  // threads
 
 template <int DT>
 EPIC_DEV void load8(const char* row, int t, int d, float (&x)[8]) {
-  if constexpr (DT == EPIC_F32) {
+  if (t >= d) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  } else if constexpr (DT == EPIC_F32) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (t + 4 * h + 4 <= d) {
@@ -82,23 +103,67 @@ EPIC_DEV void split_f16(float x, _Float16& a, _Float16& b) {
 }
 
 // Eight numbers of packed row `row` at t.
-template <int DT>
+template <int FORM>
 EPIC_DEV void store8(char* row, int64_t plane, int t, const float (&x)[8]) {
-  uint4 a;
-  if constexpr (DT == EPIC_F32) {
-    uint4 b;
-    _Float16 p[8], q[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) split_f16(x[e], p[e], q[e]);
-    a = __builtin_bit_cast(uint4, p);
-    b = __builtin_bit_cast(uint4, q);
-    *(uint4*)(row + plane + 2 * (int64_t)t) = b;
-  } else if constexpr (DT == EPIC_F16) {
-    a = make_uint4(pack_f16(x[0], x[1]), pack_f16(x[2], x[3]), pack_f16(x[4], x[5]), pack_f16(x[6], x[7]));
+  if constexpr (FORM == kFormF32) {
+    *(float4*)(row + 4 * (int64_t)t) = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)(row + 4 * (int64_t)t + 16) = make_float4(x[4], x[5], x[6], x[7]);
   } else {
-    a = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    uint4 a;
+    if constexpr (FORM == kFormSplit) {
+      _Float16 p[8], q[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) split_f16(x[e], p[e], q[e]);
+      a = __builtin_bit_cast(uint4, p);
+      *(uint4*)(row + plane + 2 * (int64_t)t) = __builtin_bit_cast(uint4, q);
+    } else if constexpr (FORM == kFormF16) {
+      a = make_uint4(pack_f16(x[0], x[1]), pack_f16(x[2], x[3]), pack_f16(x[4], x[5]), pack_f16(x[6], x[7]));
+    } else {
+      a = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+    *(uint4*)(row + 2 * (int64_t)t) = a;
   }
-  *(uint4*)(row + 2 * (int64_t)t) = a;
+}
+
+struct __attribute__((packed, aligned(2))) Loose8 {
+  uint32_t d[2];
+};
+// Four numbers at t of a row of d in the caller's memory; nothing past its end.
+template <int DT>
+EPIC_DEV void store4(char* row, int t, int d, const float (&x)[4]) {
+  if (t + 4 <= d) {
+    if constexpr (DT == EPIC_F32)
+      *(Loose16*)(row + 4 * (int64_t)t) = Loose16{{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}};
+    else if constexpr (DT == EPIC_F16)
+      *(Loose8*)(row + 2 * (int64_t)t) = Loose8{{pack_f16(x[0], x[1]), pack_f16(x[2], x[3])}};
+    else
+      *(Loose8*)(row + 2 * (int64_t)t) = Loose8{{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])}};
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (t + k < d) {
+      if constexpr (DT == EPIC_F32)
+        *(float*)(row + 4 * (int64_t)(t + k)) = x[k];
+      else
+        *(uint16_t*)(row + 2 * (int64_t)(t + k)) = (uint16_t)(DT == EPIC_F16 ? pack_f16(x[k], 0.f) : pack_bf16(x[k], 0.f));
+    }
+}
+// Eight.
+template <int DT>
+EPIC_DEV void put8(char* row, int t, int d, const float (&x)[8]) {
+  if (t + 8 <= d && DT != EPIC_F32) {
+    Loose16 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v.d[k] = DT == EPIC_F16 ? pack_f16(x[2 * k], x[2 * k + 1]) : pack_bf16(x[2 * k], x[2 * k + 1]);
+    *(Loose16*)(row + 2 * (int64_t)t) = v;
+    return;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float y[4] = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+    store4<DT>(row, t + 4 * h, d, y);
+  }
 }
 
 // The power of two that scales a largest magnitude to [2^14, 2^15).
@@ -129,61 +194,128 @@ EPIC_DEV bool kept_row(const GatherArgs& a, int r) {
 // One row to 8 bits, by a wavefront: the scale is a 127th of the largest
 // magnitude, ties go to the even number.  A row without a magnitude of 1e-30 has
 // scale 0 and no number but 0, one with a NaN or an infinity scale NaN and 0.
+// Rows of up to 4096 numbers are read once.
 template <int DT>
 EPIC_DEV void quantize_row(const char* row, int d, int8_t* out, int stride, float* scale, int lane) {
+  constexpr int N = 8;
+  float x[N][8];
   float top = 0.f;
   bool odd = false;
-  for (int t = lane * 8; t < d; t += 512) {
-    float x[8];
-    load8<DT>(row, t, d, x);
+  const auto load = [&](int t0) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      top = fmaxf(top, fabsf(x[e]));
-      odd = odd || !(fabsf(x[e]) < kInf);
-    }
+    for (int j = 0; j < N; ++j) load8<DT>(row, t0 + j * 512 + lane * 8, d, x[j]);
+  };
+  for (int t0 = 0; t0 < d; t0 += 512 * N) {
+    load(t0);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        top = fmaxf(top, fabsf(x[j][e]));
+        odd = odd || !(fabsf(x[j][e]) < kInf);
+      }
   }
   top = wave_max(top);
   odd = __ballot(odd) != 0;
   const float inv = odd || top < 1e-30f ? 0.f : 127.f / top;
   if (lane == 0) *scale = odd ? __builtin_nanf("") : inv == 0.f ? 0.f : top / 127.f;
-  for (int t = lane * 8; t < stride; t += 512) {
-    float x[8];
-    load8<DT>(row, t, d, x);
-    uint32_t q[2] = {0u, 0u};
+  for (int t0 = 0; t0 < stride; t0 += 512 * N) {
+    if (d > 512 * N) load(t0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int v = inv == 0.f ? 0 : (int)rintf(x[e] * inv);
-      q[e >> 2] |= (uint32_t)(v & 255) << (8 * (e & 3));
+    for (int j = 0; j < N; ++j) {
+      const int t = t0 + j * 512 + lane * 8;
+      uint32_t q[2] = {0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int v = inv == 0.f ? 0 : (int)rintf(x[j][e] * inv);
+        q[e >> 2] |= (uint32_t)(v & 255) << (8 * (e & 3));
+      }
+      if (t < stride) *(uint2*)(out + t) = make_uint2(q[0], q[1]);
     }
-    *(uint2*)(out + t) = make_uint2(q[0], q[1]);
   }
+}
+
+// A row to packed 16-bit numbers, multiplied with 2^e; with a second place also
+// with 2^e2.
+template <int FORM, bool TWO>
+EPIC_DEV void pack_row(const char* row, int d, char* out, char* out2, int64_t plane, int width, int e, int e2, int lane) {
+  constexpr int N = 4;  // loads ahead
+  for (int t0 = 0; t0 < width; t0 += 512 * N) {
+    float x[N][8];
+#pragma unroll
+    for (int j = 0; j < N; ++j) load8<kDtype<FORM>>(row, t0 + j * 512 + lane * 8, d, x[j]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int t = t0 + j * 512 + lane * 8;
+      if (t >= width) continue;
+      if constexpr (FORM == kFormSplit) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[j][k] = __builtin_amdgcn_ldexpf(x[j][k], e);
+      }
+      store8<FORM>(out, plane, t, x[j]);
+      if constexpr (TWO) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[j][k] = __builtin_amdgcn_ldexpf(x[j][k], e2);
+        store8<FORM>(out2, plane, t, x[j]);
+      }
+    }
+  }
+}
+
+template <int DT>
+EPIC_DEV void zero_grad(char* row, int d, int lane) {
+  const float zero[8] = {};
+  for (int t = lane * 8; t < d; t += 512) put8<DT>(row, t, d, zero);
 }
 
 enum GatherMode { kForward, kBackward, kQuantize };
 
+// Of every 64 rows of the window how many count, and the largest power of two of
+// their weights: one wavefront each.
+__global__ void __launch_bounds__(256) count_kernel(GatherArgs a) {
+  const int group = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+  const int total = a.batch * a.rows, r = group * 64 + lane;
+  if (group * 64 >= total) return;
+  const bool on = r < total && kept_row(a, r);
+  const float w = on && a.weight ? a.weight[r] : 1.f;
+  const int e = on && w != 0.f && fabsf(w) < kInf ? __builtin_amdgcn_frexp_expf(w) : -1000;
+  const int n = (int)__popcll(__ballot(on));
+  const float top = wave_max((float)e);
+  if (lane == 0) a.counts[group] = make_int2(n, (int)top);
+}
+
 // The rows that count, one after another, zeros behind them up to a multiple of
-// 64.  Every workgroup counts the rows before its own itself (4 bytes a row from
-// the L2), so that one launch does it.
-template <int DT, int MODE>
-__global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a) {
-  __shared__ int lds_n[kGather / 64];
-  __shared__ int lds_own[64];
-  __shared__ float lds_f[kGather / 64];
+// 64 (the gradients' products sum over them).  Every workgroup counts the rows
+// before its own itself, so that one launch does it for up to 1024 rows; of more it
+// adds up count_kernel's numbers of 64 rows each.
+template <int FORM, int MODE>
+EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather / 64], int (&lds_own)[64], float (&lds_f)[kGather / 64]) {
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int total = a.batch * a.rows, first = (int)blockIdx.x * a.per, last = min(total, first + a.per);
-  constexpr bool kScaled = MODE == kBackward && DT != EPIC_BF16;
+  const int total = a.batch * a.rows, first = group * a.per, last = min(total, first + a.per);
+  constexpr int DT = kDtype<FORM>;
+  constexpr bool kWeights = MODE == kBackward && kScaled<FORM>;
   int before = 0, top_exp = INT32_MIN;
   // (the powers of two of the rows' weights go by the largest one)
-  for (int r = tid; r < (kScaled ? total : first); r += kGather)
-    if (kept_row(a, r)) {
-      before += r < first;
-      if constexpr (kScaled) {
-        const float w = a.weight ? a.weight[r] : 1.f;
-        if (w != 0.f && fabsf(w) < kInf) top_exp = max(top_exp, __builtin_amdgcn_frexp_expf(w));
-      }
+  if (a.counts) {
+    const int mine = first / 64, groups = kWeights ? (total + 63) / 64 : mine;
+    for (int g = tid; g < groups; g += kGather) {
+      const int2 c = a.counts[g];
+      before += g < mine ? c.x : 0;
+      top_exp = max(top_exp, c.y);
     }
+    if (wave == 0 && mine * 64 + lane < first) before += kept_row(a, mine * 64 + lane);
+  } else {
+    for (int r = tid; r < (kWeights ? total : first); r += kGather)
+      if (kept_row(a, r)) {
+        before += r < first;
+        if constexpr (kWeights) {
+          const float w = a.weight ? a.weight[r] : 1.f;
+          if (w != 0.f && fabsf(w) < kInf) top_exp = max(top_exp, __builtin_amdgcn_frexp_expf(w));
+        }
+      }
+  }
   before = (int)wave_sum((float)(before & 0xFFF)) + ((int)wave_sum((float)(before >> 12)) << 12);
-  if constexpr (kScaled) top_exp = (int)wave_max((float)max(top_exp, -1000));
+  if constexpr (kWeights) top_exp = (int)wave_max((float)max(top_exp, -1000));
   if (lane == 0) {
     lds_n[wave] = before;
     lds_f[wave] = (float)top_exp;
@@ -191,11 +323,10 @@ __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a) {
   __syncthreads();
   before = 0;
   for (int w = 0; w < kGather / 64; ++w) before += lds_n[w];
-  if constexpr (kScaled)
+  if constexpr (kWeights)
     for (int w = 0; w < kGather / 64; ++w) top_exp = max(top_exp, (int)lds_f[w]);
-  float mine = 1.f;
   int h_exp = 0;
-  if constexpr (DT == EPIC_F32 && MODE != kQuantize) h_exp = scale_exp(top_of(a.tops, a.top_parts[0], lds_f));
+  if constexpr (FORM == kFormSplit && MODE != kQuantize) h_exp = scale_exp(top_of(a.tops, a.top_parts[0], lds_f));
   for (int base = first; base < last; base += 64) {
     const int n = min(64, last - base);
     __syncthreads();
@@ -214,24 +345,7 @@ __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a) {
         if constexpr (MODE == kForward) {
           if (lane == 0) a.loss[r] = a.lse_out[r] = 0.f;
         } else if constexpr (MODE == kBackward) {
-          if (a.grad) {
-            char* g = a.grad + b * a.grad_seq + in * a.grad_row;
-            constexpr int S = kSize<DT>;
-            const float zero[kPer<DT>] = {};
-            (void)zero;
-            for (int t = lane * kPer<DT>; t < a.d; t += 64 * kPer<DT>) {
-              if (t + kPer<DT> <= a.d) {
-                *(Loose16*)(g + (int64_t)t * S) = Loose16{{0u, 0u, 0u, 0u}};
-              } else {
-                for (int e = t; e < a.d; ++e) {
-                  if constexpr (S == 4)
-                    *(uint32_t*)(g + 4 * (int64_t)e) = 0u;
-                  else
-                    *(uint16_t*)(g + 2 * (int64_t)e) = 0;
-                }
-              }
-            }
-          }
+          if (a.grad) zero_grad<DT>(a.grad + b * a.grad_seq + in * a.grad_row, a.d, lane);
         }
         continue;
       }
@@ -246,48 +360,35 @@ __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a) {
         int shift = 0;
         if constexpr (MODE == kBackward) {
           float w = a.weight ? a.weight[r] : 1.f;
-          if (kScaled && w != 0.f && fabsf(w) < kInf) {
-            const int e = __builtin_amdgcn_frexp_expf(w);
+          int e = 0;
+          if (kWeights && w != 0.f && fabsf(w) < kInf) {
+            e = __builtin_amdgcn_frexp_expf(w);
             shift = e - top_exp;
             w = __builtin_amdgcn_frexp_mantf(w);
-            if (lane == 0) a.kept.exp[at] = e;
-          } else if (lane == 0) {
-            a.kept.exp[at] = 0;
           }
           if (lane == 0) {
+            a.kept.exp[at] = e;
             a.kept.mul[at] = y < 0 ? 0.f : w;
-            a.kept.lse[at] = a.lse[r];
+            a.kept.lse[at] = y < 0 ? 0.f : a.lse[r];
           }
         }
-        for (int t = lane * 8; t < (int)(a.stride / 2); t += 512) {
-          float x[8];
-          load8<DT>(row, t, a.d, x);
-          if constexpr (DT == EPIC_F32) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_ldexpf(x[e], h_exp);
-          }
-          store8<DT>(a.out + at * a.stride, a.plane, t, x);
-          if constexpr (kScaled) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_ldexpf(x[e], shift);
-            store8<DT>(a.out2 + at * a.stride, a.plane, t, x);
-          }
-        }
+        // a row that adds nothing has no numbers
+        pack_row<FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.out + at * a.stride, a.out2 + at * a.stride, a.plane,
+                              a.width, h_exp, shift, lane);
       }
     }
   }
-  (void)mine;
   if (last == total) {
     if (tid == 0) *a.kept.count = before;
-    if constexpr (kScaled)
+    if constexpr (kWeights)
       if (tid == 0) a.kept.count[1] = top_exp == -1000 ? 0 : top_exp;
     if constexpr (MODE == kBackward) {
       const int end = (before + 63) / 64 * 64, vecs = (int)(a.stride / 16);
       for (int i = tid; i < (end - before) * vecs; i += kGather) {
         const int64_t at = (int64_t)before * a.stride + (int64_t)i * 16;
         *(uint4*)(a.out + at) = make_uint4(0, 0, 0, 0);
-        if constexpr (kScaled) *(uint4*)(a.out2 + at) = make_uint4(0, 0, 0, 0);
-        if constexpr (DT == EPIC_F32) {
+        if constexpr (kWeights) *(uint4*)(a.out2 + at) = make_uint4(0, 0, 0, 0);
+        if constexpr (FORM == kFormSplit) {
           *(uint4*)(a.out + a.plane + at) = make_uint4(0, 0, 0, 0);
           *(uint4*)(a.out2 + a.plane + at) = make_uint4(0, 0, 0, 0);
         }
@@ -310,6 +411,7 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
   const bool head = (int)blockIdx.x >= a.g.top_parts[0];
   const int part = head ? (int)blockIdx.x - a.g.top_parts[0] : (int)blockIdx.x, parts = a.g.top_parts[head];
   const int total = head ? a.g.V : a.g.batch * a.g.rows;
+  constexpr int N = 4;  // loads ahead
   float top = 0.f;
   for (int r = part * 4 + wave; r < total; r += parts * 4) {
     const char* row;
@@ -320,12 +422,15 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
       const int b = r / a.g.rows;
       row = a.g.data + b * a.g.seq_stride + (r - b * a.g.rows) * a.g.row_stride;
     }
-    for (int t = lane * 8; t < a.g.d; t += 512) {
-      float x[8];
-      load8<EPIC_F32>(row, t, a.g.d, x);
+    for (int t0 = 0; t0 < a.g.d; t0 += 512 * N) {
+      float x[N][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (fabsf(x[e]) < kInf) top = fmaxf(top, fabsf(x[e]));
+      for (int j = 0; j < N; ++j) load8<EPIC_F32>(row, t0 + j * 512 + lane * 8, a.g.d, x[j]);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (fabsf(x[j][e]) < kInf) top = fmaxf(top, fabsf(x[j][e]));
     }
   }
   top = block_max(top, lds);
@@ -340,28 +445,36 @@ struct PackArgs {
   int V, d, v0, count;
   char* out;
   int64_t stride, plane;
+  int width;
   const float* tops;
   int top_parts[2];
 };
-template <int DT>
-__global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
-  __shared__ float lds[4];
+template <int FORM>
+EPIC_DEV void pack_rows(const PackArgs& a, int group, int groups, float* lds) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   int e_head = 0;
-  if constexpr (DT == EPIC_F32) e_head = scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
-  for (int i = (int)blockIdx.x * 4 + wave; i < a.count; i += (int)gridDim.x * 4) {
-    const char* row = a.head + (a.v0 + i) * a.head_row;
-    const int d = a.v0 + i < a.V ? a.d : 0;
-    for (int t = lane * 8; t < (int)(a.stride / 2); t += 512) {
-      float x[8];
-      load8<DT>(row, t, d, x);
-      if constexpr (DT == EPIC_F32) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_ldexpf(x[e], e_head);
-      }
-      store8<DT>(a.out + i * a.stride, a.plane, t, x);
-    }
-  }
+  if constexpr (FORM == kFormSplit) e_head = scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
+  for (int i = group * 4 + wave; i < a.count; i += groups * 4)
+    pack_row<FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.out + i * a.stride, nullptr, a.plane,
+                        a.width, e_head, 0, lane);
+}
+template <int FORM>
+__global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
+  __shared__ float lds[4];
+  pack_rows<FORM>(a, (int)blockIdx.x, (int)gridDim.x, lds);
+}
+
+// The rows that count by the first `groups` workgroups, and by the others the
+// head's first piece where it has to be packed.
+template <int FORM, int MODE>
+__global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a, PackArgs p, int groups) {
+  __shared__ int lds_n[kGather / 64];
+  __shared__ int lds_own[64];
+  __shared__ float lds_f[kGather / 64];
+  if ((int)blockIdx.x < groups)
+    gather_rows<FORM, MODE>(a, (int)blockIdx.x, lds_n, lds_own, lds_f);
+  else if constexpr (MODE != kQuantize)
+    pack_rows<FORM>(p, (int)blockIdx.x - groups, (int)gridDim.x - groups, lds_f);
 }
 
 template <int DT>
@@ -379,11 +492,11 @@ struct HeadArgs {
   Operand H, W;      // rows that count [N, d], (a piece of) the head [v, d]
   Kept kept;
   int steps;         // of d
+  int piece;         // tokens of a whole piece
+  int width;         // d up to a multiple of 64
   uint32_t pairs;
-  int planes;
   int v0, v1;        // tokens of the piece
   int V, d;
-  int first;         // workgroup of the launch
   // losses
   float2* part;      // [rows][parts] maximum and sum of a tile's columns
   int64_t parts;
@@ -395,7 +508,9 @@ struct HeadArgs {
   Operand H2;
   float* dh;         // [slices][rows][d] float32
   int64_t dh_slice;
-  int slices, add;
+  int max_slices, add, last;  // last: the piece after which gradients are whole
+  char* grad_hidden;
+  int64_t gh_seq, gh_row;  // bytes
   char* grad_head;
   int64_t grad_row;  // bytes
   // 8 bits
@@ -406,88 +521,150 @@ struct HeadArgs {
   int rows;
 };
 
+// ---- Tiles.  Three sizes, one workgroup of 512 threads a CU for all: the large
+// one takes the least from LDS and memory for a product, the smaller ones cut a
+// small result into more pieces and keep more loads of the head on their way.
+// Which, the kernel decides, by how many rows count.
+template <int KIND, bool A_ALONG, bool B_ALONG>
+struct Sizes {
+  typedef Tile<KIND, 256, 256, 2, 4, 2, A_ALONG, B_ALONG> Large;
+  typedef Tile<KIND, 128, 128, 2, 4, 4, A_ALONG, B_ALONG> Mid;
+  typedef Tile<KIND, 64, 128, 2, 4, 5, A_ALONG, B_ALONG> Few;
+};
+constexpr int kProductThreads = 512, kProductLds = 131072, kCus = 256;
+
+EPIC_DEV int ceil_div(int a, int b) { return (a + b - 1) / b; }
+// 0 large, 1 mid, 2 few: of a result of m x n sums, `copies` times.  The rounds
+// that the CUs take, by what a round of each size costs.
+template <int KIND>
+EPIC_DEV int tile_size(int m, int n, int copies = 1) {
+  const int c0 = ceil_div(ceil_div(m, 256) * ceil_div(n, 256) * copies, kCus) * (KIND == kF32 ? 32 : 20);
+  const int c1 = ceil_div(ceil_div(m, 128) * ceil_div(n, 128) * copies, kCus) * 9;
+  const int c2 = ceil_div(ceil_div(m, 64) * ceil_div(n, 128) * copies, kCus) * (KIND == kF32 ? 5 : 6);
+  return c2 < c1 && c2 < c0 ? 2 : c1 < c0 ? 1 : 0;
+}
+template <class S, class F>
+EPIC_DEV void with_size(int size, F&& f) {
+  if (size == 0) {
+    typename S::Large t;
+    f(t);
+  } else if (size == 1) {
+    typename S::Mid t;
+    f(t);
+  } else {
+    typename S::Few t;
+    f(t);
+  }
+}
+
 // What sums of products are multiplied with to be logits.
-template <bool SPLIT>
+template <int FORM>
 EPIC_DEV float unscale(const HeadArgs& a, float* lds) {
-  if constexpr (!SPLIT) return 1.f;
+  if constexpr (FORM != kFormSplit) return 1.f;
   const int e = scale_exp(top_of(a.tops, a.top_parts[0], lds)) + scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
   return __builtin_amdgcn_ldexpf(1.f, -e);
 }
 
-// A tile's columns to a maximum and a sum for every row, over two wavefronts or
-// more by LDS, and the logit of the row's token.
-template <class T, bool SPLIT>
-__global__ void __launch_bounds__(T::kThreads) lse_kernel(HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ float lds_top[4];
-  const int count = *a.kept.count, m = (count + T::BM - 1) / T::BM, n = (a.v1 - a.v0 + T::BN - 1) / T::BN;
-  const int id = a.first + (int)blockIdx.x;
-  if (id >= m * n) return;
-  int tm, tn;
-  tile_of(id, m, n, tm, tn);
-  T t;
-  t.run(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, SPLIT ? 3 : 1, a.pairs, smem);
-  const float by = unscale<SPLIT>(a, lds_top);
-  __syncthreads();
-  float2* part = (float2*)smem;  // [WN][BM]
-  const int wn = T::wave() % T::WN, lane = (int)threadIdx.x & 63;
+// A tile's columns to a maximum and a sum for every row, over the wavefronts of a
+// row of tiles by LDS, and the logit of the row's token.  exp2 takes one product
+// and sum: with c = log2(e) (and what unscales sums) t c is rounded to T, and the
+// sum of 2^(l c - T) is too large by the factor 2^(t c - T), which is taken out.
+template <int FORM, class T>
+EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem, float2* part, int (&target)[2][256]) {
+  const int m = ceil_div(count, T::BM), n = ceil_div(a.v1 - a.v0, T::BN);
+  const float c = by * kLog2e;
+  auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
+  every_tile<kPairs<FORM>>(
+      t, smem, [&](int i) { return dealt(i, m * n); },
+      [&](int id) {
+        int tm, tn;
+        place(id, tm, tn);
+        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, a.pairs);
+      },
+      [&](int id, int k) {
+        int tm, tn;
+        place(id, tm, tn);
+        for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
+          const int at = tm * T::BM + r;
+          target[k][r] = at < count ? a.kept.target[at] - a.v0 - tn * T::BN : -1;
+        }
+      },
+      [&](int id, int k) {
+        int tm, tn;
+        place(id, tm, tn);
+        const int wn = T::wave() % T::WN, lane = T::lane_now();
+        const int cols = a.v1 - a.v0 - tn * T::BN;  // that there are, from the tile's first on
 #pragma unroll
-  for (int i = 0; i < T::MT; ++i) {
-    const int r = T::row(i), at = tm * T::BM + r;
-    const int y = at < count ? a.kept.target[at] : -1;
-    float top = -kInf;
+        for (int i = 0; i < T::MT; ++i) {
+          const int r = T::row(i, lane), y = target[k][r];
+          if (cols < T::BN) {
 #pragma unroll
-    for (int j = 0; j < T::NT; ++j)
+            for (int j = 0; j < T::NT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int v = a.v0 + tn * T::BN + T::col(j) + e;
-        float l = t.acc[i][j][e] * by;
-        l = v < a.v1 ? l : -kInf;
-        t.acc[i][j][e] = l;
-        if (v == y) a.at_target[at] = l;
-        top = fmaxf(top, l);
-      }
-    const float base = top > -kInf ? top : 0.f;
-    float sum = 0.f;
+              for (int e = 0; e < 4; ++e) t.acc[i][j][e] = T::col(j, lane) + e < cols ? t.acc[i][j][e] : -kInf;
+          }
+          if (__any((unsigned)(y - wn * (T::BN / T::WN)) < (unsigned)(T::BN / T::WN))) {
 #pragma unroll
-    for (int j = 0; j < T::NT; ++j)
+            for (int j = 0; j < T::NT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((t.acc[i][j][e] - base) * kLog2e);
-    // the four lanes of a row
+              for (int e = 0; e < 4; ++e)
+                if (T::col(j, lane) + e == y) a.at_target[tm * T::BM + r] = t.acc[i][j][e] * by;
+          }
+          float top = -kInf;
 #pragma unroll
-    for (int s = 16; s < 64; s *= 2) {
-      const float t2 = __shfl_xor(top, s), s2 = __shfl_xor(sum, s);
-      const float both = fmaxf(top, t2), b2 = both > -kInf ? both : 0.f;
-      sum = sum * __builtin_amdgcn_exp2f((top - b2) * kLog2e) + s2 * __builtin_amdgcn_exp2f((t2 - b2) * kLog2e);
-      top = both;
-    }
-    if (lane < 16) part[wn * T::BM + r] = make_float2(top, sum);
-  }
-  __syncthreads();
-  for (int r = (int)threadIdx.x; r < T::BM; r += T::kThreads) {
-    if (tm * T::BM + r >= count) continue;
-    float2 p = part[r];
-    for (int w = 1; w < T::WN; ++w) {
-      const float2 q = part[w * T::BM + r];
-      const float both = fmaxf(p.x, q.x), b2 = both > -kInf ? both : 0.f;
-      p.y = p.y * __builtin_amdgcn_exp2f((p.x - b2) * kLog2e) + q.y * __builtin_amdgcn_exp2f((q.x - b2) * kLog2e);
-      p.x = both;
-    }
-    a.part[(int64_t)(tm * T::BM + r) * a.parts + a.v0 / T::BN + tn] = p;
-  }
+          for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, t.acc[i][j][e]);
+          top = fmaxf(top, __shfl_xor(top, 16));  // the four lanes of a row
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float base = top > -kInf ? top : 0.f, tc = base * c;
+          float sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][e], c, -tc));
+          sum += __shfl_xor(sum, 16);
+          sum += __shfl_xor(sum, 32);
+          if (lane < 16) part[wn * T::BM + r] = make_float2(top * by, sum * __builtin_amdgcn_exp2f(-__builtin_fmaf(base, c, -tc)));
+        }
+        lds_barrier();
+        for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
+          if (tm * T::BM + r >= count) continue;
+          float2 p = part[r];
+          for (int w = 1; w < T::WN; ++w) {
+            const float2 q = part[w * T::BM + r];
+            const float both = fmaxf(p.x, q.x), b2 = both > -kInf ? both : 0.f;
+            p.y = p.y * __builtin_amdgcn_exp2f((p.x - b2) * kLog2e) + q.y * __builtin_amdgcn_exp2f((q.x - b2) * kLog2e);
+            p.x = both;
+          }
+          a.part[(int64_t)(tm * T::BM + r) * a.parts + a.v0 / T::BN + tn] = p;
+        }
+      });
+}
+template <int FORM>
+__global__ void __launch_bounds__(kProductThreads) lse_kernel(HeadArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kProductLds];
+  __shared__ float lds_top[kProductThreads / 64];
+  __shared__ float2 part[4 * 256];
+  __shared__ int target[2][256];
+  const int count = *a.kept.count;
+  const float by = unscale<FORM>(a, lds_top);
+  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { lse_tiles<FORM>(a, t, count, by, smem, part, target); });
 }
 
 // Losses from the tiles' maxima and sums, one wavefront a row.
+template <int FORM>
 __global__ void __launch_bounds__(256) loss_kernel(HeadArgs a, float* loss, float* lse_out) {
-  const int at = a.first + (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+  const int at = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   if (at >= *a.kept.count) return;
   const float2* p = a.part + at * a.parts;
+  const int parts = ceil_div(a.V, tile_size<kKind<FORM>>(*a.kept.count, a.piece) == 0 ? 256 : 128);
   float top = -kInf;
-  for (int64_t i = lane; i < a.parts; i += 64) top = fmaxf(top, p[i].x);
+  for (int i = lane; i < parts; i += 64) top = fmaxf(top, p[i].x);
   top = wave_max(top);
   const float base = top > -kInf ? top : 0.f;
   float sum = 0.f;
-  for (int64_t i = lane; i < a.parts; i += 64) sum += p[i].y * __builtin_amdgcn_exp2f((p[i].x - base) * kLog2e);
+  for (int i = lane; i < parts; i += 64) sum += p[i].y * __builtin_amdgcn_exp2f((p[i].x - base) * kLog2e);
   sum = wave_sum(sum);
   if (lane == 0) {
     const int y = a.kept.target[at], r = a.kept.src[at];
@@ -499,287 +676,386 @@ __global__ void __launch_bounds__(256) loss_kernel(HeadArgs a, float* loss, floa
 
 // (p - y) times the rows' weights, in 16 bits (two planes where inputs have 32).
 // float16 has few small numbers, so there p is multiplied with 2^14 and the
-// weights are in [1/2, 1): 2^-24 of p = 1 is a normal number.  Rows past the last
-// up to a multiple of 64 and columns past the vocabulary are zeros, which the
-// products that follow sum over.
-template <class T, bool SPLIT>
-__global__ void __launch_bounds__(T::kThreads) excess_kernel(HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ float lds_top[4];
-  const int count = *a.kept.count, m = (count + T::BM - 1) / T::BM, n = (a.v1 - a.v0 + T::BN - 1) / T::BN;
-  const int id = a.first + (int)blockIdx.x;
-  if (id >= m * n) return;
-  int tm, tn;
-  tile_of(id, m, n, tm, tn);
-  T t;
-  t.run(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, SPLIT ? 3 : 1, a.pairs, smem);
-  const float by = unscale<SPLIT>(a, lds_top);
-  constexpr float kScale = T::KIND == kF16 ? 16384.f : 1.f;
-#pragma unroll
-  for (int i = 0; i < T::MT; ++i) {
-    const int at = tm * T::BM + T::row(i);
-    const bool on = at < count;
-    const int y = on ? a.kept.target[at] : -2;
-    const float lse = on ? a.kept.lse[at] : 0.f, mul = on ? a.kept.mul[at] * kScale : 0.f;
-    char* row = const_cast<char*>(a.G.data) + at * a.G.stride;
-#pragma unroll
-    for (int j = 0; j < T::NT; j += T::F) {
-      float g[4 * T::F];
-#pragma unroll
-      for (int f = 0; f < T::F; ++f)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int v = a.v0 + tn * T::BN + T::col(j + f) + e;
-          const float x = t.acc[i][j + f][e] * by - lse;
-          float p = __builtin_amdgcn_exp2f(x * kLog2e);
-          if (v == y) p = expm1f(x);  // 1 - p without what p = 1 rounds away
-          g[4 * f + e] = y == -2 || v >= a.v1 ? 0.f : p * mul;
+// weights are in [1/2, 1): 2^-24 of p = 1 is a normal number.  Numbers of rows past
+// the last, of rows without a token (which have hidden states 0 and weight 0) and
+// of columns past the vocabulary are 0: the products that follow sum over them.
+template <int FORM, class T>
+EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* smem, int (&target)[2][256], float2 (&scale)[2][256]) {
+  constexpr float kScale = kScaled<FORM> ? 16384.f : 1.f;
+  const int m = ceil_div(count, T::BM), n = ceil_div(a.v1 - a.v0, T::BN);
+  const float c = by * kLog2e;
+  auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
+  every_tile<kPairs<FORM>>(
+      t, smem, [&](int i) { return dealt(i, m * n); },
+      [&](int id) {
+        int tm, tn;
+        place(id, tm, tn);
+        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, a.pairs);
+      },
+      [&](int id, int k) {
+        int tm, tn;
+        place(id, tm, tn);
+        for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
+          const int at = tm * T::BM + r;
+          int y = -1;
+          float2 x = make_float2(0.f, 0.f);
+          if (at < count) {
+            y = a.kept.target[at] - a.v0 - tn * T::BN;
+            const float lse = a.kept.lse[at];
+            x.x = lse * kLog2e;  // rounded; the factor below has what is left out
+            x.y = a.kept.mul[at] * kScale * __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, kLog2e, -x.x));
+          }
+          target[k][r] = y;
+          scale[k][r] = x;
         }
-      char* to = row + 2 * (tn * T::BN + T::col(j));
+      },
+      [&](int id, int k) {
+        int tm, tn;
+        place(id, tm, tn);
+        const int wn = T::wave() % T::WN, lane = T::lane_now();
+        const int cols = a.v1 - a.v0 - tn * T::BN;
 #pragma unroll
-      for (int h = 0; h < 4 * T::F; h += 8) {
-        if constexpr (T::F == 1) {
-          static_assert(T::F > 1);
-        } else {
-          const float x[8] = {g[h], g[h + 1], g[h + 2], g[h + 3], g[h + 4], g[h + 5], g[h + 6], g[h + 7]};
-          store8<SPLIT ? EPIC_F32 : T::KIND == kF16 ? EPIC_F16 : EPIC_BF16>(to, a.G.plane, h, x);
+        for (int i = 0; i < T::MT; ++i) {
+          const int r = T::row(i, lane), at = tm * T::BM + r, y = target[k][r];
+          const float2 x = scale[k][r];
+          char* row = const_cast<char*>(a.G.data) + at * a.G.stride + 2 * (int64_t)(tn * T::BN);
+          const bool some = __any((unsigned)(y - wn * (T::BN / T::WN)) < (unsigned)(T::BN / T::WN));
+#pragma unroll
+          for (int j = 0; j < T::NT; j += T::F) {
+            float g[4 * T::F];
+#pragma unroll
+            for (int f = 0; f < 4 * T::F; ++f)
+              g[f] = x.y * __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j + f / 4][f & 3], c, -x.x));
+            const int c0 = T::col(j, lane);
+            if (some) {
+#pragma unroll
+              for (int f = 0; f < 4 * T::F; ++f)
+                if (c0 + f == y)  // 1 - p without what p = 1 rounds away
+                  g[f] = a.kept.mul[at] * kScale * expm1f(t.acc[i][j + f / 4][f & 3] * by - a.kept.lse[at]);
+            }
+            if (cols < T::BN || (tm + 1) * T::BM > count) {
+#pragma unroll
+              for (int f = 0; f < 4 * T::F; ++f) g[f] = c0 + f < cols && at < count ? g[f] : 0.f;
+            }
+#pragma unroll
+            for (int h = 0; h < 4 * T::F; h += 8) {
+              const float v[8] = {g[h], g[h + 1], g[h + 2], g[h + 3], g[h + 4], g[h + 5], g[h + 6], g[h + 7]};
+              store8<FORM>(row + 2 * c0, a.G.plane, h, v);
+            }
+          }
         }
-      }
-    }
-  }
+      });
+}
+template <int FORM>
+__global__ void __launch_bounds__(kProductThreads) excess_kernel(HeadArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kProductLds];
+  __shared__ float lds_top[kProductThreads / 64];
+  __shared__ int target[2][256];
+  __shared__ float2 scale[2][256];  // lse in powers of two, and what 2^(l - lse) is multiplied with
+  const int count = *a.kept.count;
+  const float by = unscale<FORM>(a, lds_top);
+  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { excess_tiles<FORM>(a, t, count, by, smem, target, scale); });
 }
 
-// A slice of the piece's part of the hidden states' gradient: G W, summed over
-// pieces in float32.
-template <class T, bool SPLIT>
-__global__ void __launch_bounds__(T::kThreads) grad_hidden_kernel(HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int count = *a.kept.count, m = (count + T::BM - 1) / T::BM, n = (a.d + T::BN - 1) / T::BN;
-  int id = a.first + (int)blockIdx.x;
-  if (id >= m * n * a.slices) return;
-  const int slice = id / (m * n);
-  id -= slice * m * n;
-  int tm, tn;
-  tile_of(id, m, n, tm, tn);
-  const int all = (a.v1 - a.v0 + 63) / 64, k0 = (int)((int64_t)all * slice / a.slices), k1 = (int)((int64_t)all * (slice + 1) / a.slices);
-  T t;
-  t.run(a.G, a.W, tm * T::BM, tn * T::BN, m * T::BM, (int)(a.H.stride / 2), k0, k1 - k0, SPLIT ? 3 : 1, a.pairs, smem);
-  const int dp = (int)(a.H.stride / 2);
+// ---- The two products with G, in one launch: the hidden states' gradient G W
+// (few tiles, long sums over the piece's tokens, cut into slices) and the head's,
+// G^T H (many tiles, sums over the rows that count).  Each workgroup takes its
+// share of the first, and of the second those that had less before first one or
+// more, so that all end at about the same time.
+struct Split {
+  int size_h, size_w;    // tiles
+  int m_h, n_h, m_w, n_w;
+  int slices;            // of the sums over tokens
+  int lead;              // tiles of the second that a workgroup with one less of the first takes before
+};
+template <int KIND>
+EPIC_DEV Split split_of(const HeadArgs& a, int count) {
+  Split s;
+  s.size_h = tile_size<KIND>(count, a.d, min(a.max_slices, max(1, a.piece / 2048)));
+  s.size_w = tile_size<KIND>(a.piece, a.d);
+  const int hm = s.size_h == 0 ? 256 : s.size_h == 1 ? 128 : 64, hn = s.size_h == 0 ? 256 : 128;
+  const int wm = s.size_w == 0 ? 256 : s.size_w == 1 ? 128 : 64, wn = s.size_w == 0 ? 256 : 128;
+  s.m_h = ceil_div(count, hm);
+  s.n_h = ceil_div(a.d, hn);
+  s.m_w = ceil_div(a.v1 - a.v0, wm);
+  s.n_w = ceil_div(a.d, wn);
+  // in steps of a 64 x 128 tile; a tile's start and end are worth some
+  const int k_h = ceil_div(a.piece, 64), k_w = ceil_div(count, 64) + 8, area_h = hm * hn / 8192, area_w = wm * wn / 8192;
+  const int64_t all = (a.grad_hidden ? (int64_t)s.m_h * s.n_h * k_h * area_h : 0) +
+                      (a.grad_head ? (int64_t)ceil_div(a.piece, wm) * s.n_w * k_w * area_w : 0);
+  s.slices = 1;
+  while (2 * s.slices <= a.max_slices && k_h >= 32 * s.slices &&
+         (int64_t)k_h * area_h * 4 * kCus > 3 * all * s.slices)
+    s.slices *= 2;
+  s.lead = (int)(((int64_t)k_h / s.slices + 8) * area_h / (k_w * area_w));
+  return s;
+}
+
+// Slices are float32, summed over pieces; of one slice, the last piece's end
+// rounds and writes the gradient.
+template <int FORM, class T>
+EPIC_DEV void grad_hidden_tiles(const HeadArgs& a, T& t, const Split& s, int count, int e, char* smem) {
+  constexpr int P = kPairs<FORM>, DT = kDtype<FORM>;
+  const int m = s.m_h, n = s.n_h, all = ceil_div(a.v1 - a.v0, 64), dp = a.width;
+  auto place = [&](int id, int& tm, int& tn) {
+    const int slice = id / (m * n);
+    tile_of(id - slice * m * n, m, n, tm, tn);
+    return slice;
+  };
+  every_tile<P>(
+      t, smem, [&](int i) { return dealt(i, m * n * s.slices); },
+      [&](int id) {
+        int tm, tn;
+        const int slice = place(id, tm, tn);
+        const int k0 = (int)((int64_t)all * slice / s.slices), k1 = (int)((int64_t)all * (slice + 1) / s.slices);
+        t.template start<P>(a.G, a.W, tm * T::BM, tn * T::BN, m * T::BM, dp, k0, k1 - k0, a.pairs);
+      },
+      [](int, int) {},
+      [&](int id, int) {
+        int tm, tn;
+        const int slice = place(id, tm, tn), lane = T::lane_now();
+        const bool whole = a.last && s.slices == 1;
 #pragma unroll
-  for (int i = 0; i < T::MT; ++i) {
-    const int at = tm * T::BM + T::row(i);
-    if (at >= count) continue;
+        for (int i = 0; i < T::MT; ++i) {
+          const int at = tm * T::BM + T::row(i, lane);
+          if (at >= count) continue;
+          char* row = nullptr;
+          int x = 0;
+          if (whole) {
+            const int r = a.kept.src[at], b = r / a.rows;
+            row = a.grad_hidden + b * a.gh_seq + (r - b * a.rows) * a.gh_row;
+            if constexpr (kScaled<FORM>) x = a.kept.exp[at] + e;
+          }
 #pragma unroll
-    for (int j = 0; j < T::NT; ++j) {
-      const int c = tn * T::BN + T::col(j);
-      if (c >= dp) continue;
-      f4* to = (f4*)(a.dh + slice * a.dh_slice + (int64_t)at * dp + c);
-      *to = a.add ? *to + t.acc[i][j] : t.acc[i][j];
-    }
+          for (int j = 0; j < T::NT; ++j) {
+            const int c = tn * T::BN + T::col(j, lane);
+            if (c >= dp) continue;
+            f4* to = (f4*)(a.dh + slice * a.dh_slice + (int64_t)at * dp + c);
+            f4 sum = t.acc[i][j];
+            if (a.add) sum += *to;
+            if (whole) {
+              float g[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) g[k] = !kScaled<FORM> ? sum[k] : __builtin_amdgcn_ldexpf(sum[k], x);
+              store4<DT>(row, c, a.d, g);
+            } else {
+              *to = sum;
+            }
+          }
+        }
+      });
+}
+
+// Rounded once.
+template <int FORM, class T>
+EPIC_DEV void grad_head_tiles(const HeadArgs& a, T& t, const Split& s, int count, int e, int first_tiles, char* smem) {
+  constexpr int P = kPairs<FORM>, DT = kDtype<FORM>;
+  const int m = s.m_w, n = s.n_w, grid = (int)gridDim.x, heavy = first_tiles % grid;
+  // of the grid's workgroups, the first `heavy` have one tile more behind them:
+  // the others take `lead` tiles each, then all in turn
+  const int light = heavy ? grid - heavy : 0, lead = min(s.lead, light ? m * n / light : 0), base = light * lead;
+  const int mine = (int)blockIdx.x - heavy;
+  auto number = [&](int i) {
+    int id;
+    if (light && mine >= 0 && i < lead)
+      id = mine + i * light;
+    else
+      id = base + (int)blockIdx.x + (i - (light && mine >= 0 ? lead : 0)) * grid;
+    return id < m * n ? id : -1;
+  };
+  every_tile<P>(
+      t, smem, number,
+      [&](int id) {
+        int tm, tn;
+        tile_of(id, m, n, tm, tn);
+        t.template start<P>(a.G, a.H2, tm * T::BM, tn * T::BN, m * T::BM, a.width, 0, ceil_div(count, 64), a.pairs);
+      },
+      [](int, int) {},
+      [&](int id, int) {
+        int tm, tn;
+        tile_of(id, m, n, tm, tn);
+        const int lane = T::lane_now();
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+          const int v = a.v0 + tm * T::BM + T::row(i, lane);
+          if (v >= a.v1) continue;
+          char* row = a.grad_head + v * a.grad_row;
+#pragma unroll
+          for (int j = 0; j < T::NT; ++j) {
+            const int c = tn * T::BN + T::col(j, lane);
+            float g[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) g[k] = !kScaled<FORM> ? t.acc[i][j][k] : __builtin_amdgcn_ldexpf(t.acc[i][j][k], e);
+            store4<DT>(row, c, a.d, g);
+          }
+        }
+      });
+}
+
+template <int FORM>
+__global__ void __launch_bounds__(kProductThreads) grad_kernel(HeadArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kProductLds];
+  __shared__ float lds_top[kProductThreads / 64];
+  constexpr int KIND = kKind<FORM>;
+  const int count = *a.kept.count;
+  const Split s = split_of<kKind<FORM>>(a, count);
+  int e_h = 0, e_w = 0;  // what takes the scales out of the sums
+  if constexpr (FORM == kFormF16) e_h = -14, e_w = a.kept.count[1] - 14;
+  if constexpr (FORM == kFormSplit) {
+    e_h = -14 - scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds_top));
+    e_w = a.kept.count[1] - 14 - scale_exp(top_of(a.tops, a.top_parts[0], lds_top));
   }
+  int first_tiles = 0;
+  if (a.grad_hidden) {
+    first_tiles = s.m_h * s.n_h * s.slices;
+    with_size<Sizes<KIND, true, false>>(s.size_h, [&](auto& t) { grad_hidden_tiles<FORM>(a, t, s, count, e_h, smem); });
+  }
+  lds_barrier();  // the last tile's numbers are read
+  if (a.grad_head)
+    with_size<Sizes<KIND, false, false>>(s.size_w, [&](auto& t) { grad_head_tiles<FORM>(a, t, s, count, e_w, first_tiles, smem); });
 }
 
 // Slices of the hidden states' gradient to its rows, one wavefront a row.
-template <int DT>
-__global__ void __launch_bounds__(256) scatter_kernel(HeadArgs a, char* grad, int64_t grad_seq, int64_t grad_row) {
+template <int FORM>
+__global__ void __launch_bounds__(256) scatter_kernel(HeadArgs a) {
+  constexpr int DT = kDtype<FORM>;
   __shared__ float lds[4];
+  const int slices = split_of<kKind<FORM>>(a, *a.kept.count).slices;
+  if (slices == 1) return;  // written already
   int e_head = 0;
-  if constexpr (DT == EPIC_F32) e_head = -scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
-  const int at = a.first + (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+  if constexpr (FORM == kFormSplit) e_head = -scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
+  const int at = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   if (at >= *a.kept.count) return;
   const int r = a.kept.src[at], b = r / a.rows;
-  char* row = grad + b * grad_seq + (r - b * a.rows) * grad_row;
-  const int dp = (int)(a.H.stride / 2);
-  const int e = DT == EPIC_BF16 ? 0 : a.kept.exp[at] - 14 + e_head;
+  char* row = a.grad_hidden + b * a.gh_seq + (r - b * a.rows) * a.gh_row;
+  const int dp = a.width;
+  const int e = !kScaled<FORM> ? 0 : a.kept.exp[at] - 14 + e_head;
   for (int t = lane * 8; t < a.d; t += 512) {
     float x[8] = {};
-    for (int s = 0; s < a.slices; ++s) {
+    for (int s = 0; s < slices; ++s) {
       const f4* p = (const f4*)(a.dh + s * a.dh_slice + (int64_t)at * dp + t);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] += p[k >> 2][k & 3];
     }
-    if constexpr (DT != EPIC_BF16) {
+    if constexpr (kScaled<FORM>) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = __builtin_amdgcn_ldexpf(x[k], e);
     }
-    if (t + 8 <= a.d) {
-      if constexpr (DT == EPIC_F32) {
-        Loose16 v[2];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k >> 2].d[k & 3] = __float_as_uint(x[k]);
-        *(Loose16*)(row + 4 * (int64_t)t) = v[0];
-        *(Loose16*)(row + 4 * (int64_t)t + 16) = v[1];
-      } else {
-        Loose16 v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          v.d[k] = DT == EPIC_F16 ? pack_f16(x[2 * k], x[2 * k + 1]) : pack_bf16(x[2 * k], x[2 * k + 1]);
-        *(Loose16*)(row + 2 * (int64_t)t) = v;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (t + k < a.d) {
-          if constexpr (DT == EPIC_F32)
-            *(float*)(row + 4 * (int64_t)(t + k)) = x[k];
-          else
-            *(uint16_t*)(row + 2 * (int64_t)(t + k)) = (uint16_t)(DT == EPIC_F16 ? pack_f16(x[k], 0.f) : pack_bf16(x[k], 0.f));
-        }
-    }
-  }
-}
-
-// The head's gradient of a piece: G^T H over the rows that count, rounded once.
-template <class T, bool SPLIT, int DT>
-__global__ void __launch_bounds__(T::kThreads) grad_head_kernel(HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ float lds_top[4];
-  const int count = *a.kept.count, m = (a.v1 - a.v0 + T::BM - 1) / T::BM, n = (a.d + T::BN - 1) / T::BN;
-  const int id = a.first + (int)blockIdx.x;
-  if (id >= m * n) return;
-  int tm, tn;
-  tile_of(id, m, n, tm, tn);
-  T t;
-  t.run(a.G, a.H2, tm * T::BM, tn * T::BN, m * T::BM, (int)(a.H.stride / 2), 0, (count + 63) / 64, SPLIT ? 3 : 1, a.pairs, smem);
-  int e = 0;
-  if constexpr (DT == EPIC_F16) e = a.kept.count[1] - 14;
-  if constexpr (DT == EPIC_F32) e = a.kept.count[1] - 14 - scale_exp(top_of(a.tops, a.top_parts[0], lds_top));
-#pragma unroll
-  for (int i = 0; i < T::MT; ++i) {
-    const int v = a.v0 + tm * T::BM + T::row(i);
-    if (v >= a.v1) continue;
-    char* row = a.grad_head + v * a.grad_row;
-#pragma unroll
-    for (int j = 0; j < T::NT; ++j) {
-      const int c = tn * T::BN + T::col(j);
-      float x[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = DT == EPIC_BF16 ? t.acc[i][j][k] : __builtin_amdgcn_ldexpf(t.acc[i][j][k], e);
-      struct __attribute__((packed, aligned(2))) Loose8 {
-        uint32_t d[2];
-      };
-      if (c + 4 <= a.d) {
-        if constexpr (DT == EPIC_F32)
-          *(Loose16*)(row + 4 * (int64_t)c) =
-              Loose16{{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}};
-        else if constexpr (DT == EPIC_F16)
-          *(Loose8*)(row + 2 * (int64_t)c) = Loose8{{pack_f16(x[0], x[1]), pack_f16(x[2], x[3])}};
-        else
-          *(Loose8*)(row + 2 * (int64_t)c) = Loose8{{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])}};
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (c + k < a.d) {
-            if constexpr (DT == EPIC_F32)
-              *(float*)(row + 4 * (int64_t)(c + k)) = x[k];
-            else
-              *(uint16_t*)(row + 2 * (int64_t)(c + k)) = (uint16_t)(DT == EPIC_F16 ? pack_f16(x[k], 0.f) : pack_bf16(x[k], 0.f));
-          }
-      }
-    }
+    put8<DT>(row, t, a.d, x);
   }
 }
 
 // Logits of a head in 8 bits: sums of whole numbers, exact in 32 bits, times the
 // row's and the token's scale.
-template <class T, int DT>
-__global__ void __launch_bounds__(T::kThreads) logits_kernel(HeadArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int count = *a.kept.count, m = (count + T::BM - 1) / T::BM, n = (a.V + T::BN - 1) / T::BN;
-  const int id = a.first + (int)blockIdx.x;
-  if (id >= m * n) return;
-  int tm, tn;
-  tile_of(id, m, n, tm, tn);
-  T t;
-  t.run(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.V, 0, a.steps, 1, 0, smem);
-#pragma unroll
-  for (int i = 0; i < T::MT; ++i) {
-    const int at = tm * T::BM + T::row(i);
-    if (at >= count) continue;
-    const int r = a.kept.src[at], b = r / a.rows;
-    const float s = a.row_scale[at];
-    char* row = a.logits + b * a.seq_stride + (r - b * a.rows) * a.row_stride;
-#pragma unroll
-    for (int j = 0; j < T::NT; j += T::F) {
-      const int c = tn * T::BN + T::col(j);
-#pragma unroll
-      for (int h = 0; h < 4 * T::F; h += kPer<DT>) {
-        float x[kPer<DT>];
-        if (c + h >= a.V) continue;
-#pragma unroll
-        for (int k = 0; k < kPer<DT>; ++k)
-          x[k] = (float)t.acc[i][j + (h + k) / 4][(h + k) & 3] * s * a.col_scale[min(c + h + k, a.V - 1)];
-        if constexpr (DT == EPIC_F16) {
-          // the product is a float32 number before it is rounded to float16: the compiler would join the two
-#pragma unroll
-          for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(x[k]));
+template <int DT, class T>
+EPIC_DEV void logits_tiles(const HeadArgs& a, T& t, int count, char* smem, int64_t (&rows)[2][256], float (&row_scale)[2][256],
+                           float (&col_scale)[2][256]) {
+  const int m = ceil_div(count, T::BM), n = ceil_div(a.V, T::BN);
+  auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
+  every_tile<1>(
+      t, smem, [&](int i) { return dealt(i, m * n); },
+      [&](int id) {
+        int tm, tn;
+        place(id, tm, tn);
+        t.template start<1>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.V, 0, a.steps, 0);
+      },
+      [&](int id, int k) {
+        int tm, tn;
+        place(id, tm, tn);
+        for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
+          const int at = tm * T::BM + r;
+          const int x = at < count ? a.kept.src[at] : 0, b = x / a.rows;
+          rows[k][r] = at < count ? b * a.seq_stride + (x - b * a.rows) * a.row_stride : -1;
+          row_scale[k][r] = at < count ? a.row_scale[at] : 0.f;
         }
-        if (c + h + kPer<DT> <= a.V) {
-          Loose16 v;
+        for (int r = T::wave() * 64 + T::lane_now(); r < T::BN; r += T::kThreads)
+          col_scale[k][r] = tn * T::BN + r < a.V ? a.col_scale[tn * T::BN + r] : 0.f;
+      },
+      [&](int id, int k) {
+        int tm, tn;
+        place(id, tm, tn);
+        const int lane = T::lane_now();
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if constexpr (DT == EPIC_F32)
-              v.d[k] = __float_as_uint(x[k]);
-            else
-              v.d[k] = DT == EPIC_F16 ? pack_f16(x[2 * k], x[2 * k + 1]) : pack_bf16(x[2 * k], x[2 * k + 1]);
-          }
-          *(Loose16*)(row + (int64_t)(c + h) * kSize<DT>) = v;
-        } else {
+        for (int j = 0; j < T::NT; j += T::F) {
+          float sc[4 * T::F];
 #pragma unroll
-          for (int k = 0; k < kPer<DT>; ++k)
-            if (c + h + k < a.V) {
-              if constexpr (DT == EPIC_F32)
-                *(float*)(row + 4 * (int64_t)(c + h + k)) = x[k];
-              else
-                *(uint16_t*)(row + 2 * (int64_t)(c + h + k)) = (uint16_t)(DT == EPIC_F16 ? pack_f16(x[k], 0.f) : pack_bf16(x[k], 0.f));
+          for (int f = 0; f < 4 * T::F; ++f) sc[f] = col_scale[k][T::col(j, lane) + f];
+          const int c = tn * T::BN + T::col(j, lane);
+#pragma unroll
+          for (int i = 0; i < T::MT; ++i) {
+            const int64_t at = rows[k][T::row(i, lane)];
+            const float s = row_scale[k][T::row(i, lane)];
+            if (at < 0) continue;
+#pragma unroll
+            for (int h = 0; h < 4 * T::F; h += 8) {
+              float x[8];
+#pragma unroll
+              for (int f = 0; f < 8; ++f) {
+                x[f] = (float)t.acc[i][j + (h + f) / 4][f & 3] * s * sc[h + f];
+                // a float32 number before it is rounded to float16: the compiler would join the two
+                if constexpr (DT == EPIC_F16) asm volatile("" : "+v"(x[f]));
+              }
+              put8<DT>(a.logits + at, c + h, a.V, x);
             }
+          }
         }
-      }
-    }
-  }
+      });
+}
+template <int DT>
+__global__ void __launch_bounds__(kProductThreads) logits_kernel(HeadArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kProductLds];
+  __shared__ int64_t rows[2][256];
+  __shared__ float row_scale[2][256], col_scale[2][256];
+  const int count = *a.kept.count;
+  with_size<Sizes<kI8, true, true>>(tile_size<kI8>(count, a.V), [&](auto& t) { logits_tiles<DT>(a, t, count, smem, rows, row_scale, col_scale); });
 }
 
 // ------------------------------------------------------------ host side
 constexpr int64_t kMaxRows = 1 << 24;
 constexpr int kMaxWidth = 65536;
-constexpr int kTopParts = 256;  // workgroups that look for a tensor's largest magnitude, at most
+constexpr int kTopParts = 2048;  // workgroups that look for a tensor's largest magnitude, at most
 
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-template <int KIND>
-using Large = Tile<KIND, 256, 256, 2, 4, 2, true, true>;
-template <int KIND>
-using Small = Tile<KIND, 64, 64, 2, 2, 4, true, true>;
-
-template <class T, class K>
-epic_status launch_tiles(K kernel, HeadArgs a, int64_t blocks, hipStream_t stream) {
-  // a launch needs to be told once that it may use more than 64 KiB of LDS
-  if (T::kLds > 65536 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds) != hipSuccess)
-    return EPIC_ERR_HIP;
-  if (blocks > INT32_MAX) return EPIC_ERR_UNSUPPORTED;
-  launches((int)blocks, T::kThreads, [&](int first, int count) {
-    a.first = first;
-    hipLaunchKernelGGL(kernel, dim3(count), dim3(T::kThreads), T::kLds, stream, a);
-  });
-  return EPIC_OK;
+// Workgroups that take one tile after another: one a CU.
+template <class K>
+void launch_product(K kernel, const HeadArgs& a, int64_t tiles, hipStream_t stream) {
+  if (tiles > 0)
+    hipLaunchKernelGGL(kernel, dim3((int)std::min<int64_t>(tiles, kCus)), dim3(kProductThreads), 0, stream, a);
 }
+// The smallest tiles of m x n sums.
+inline int64_t most_tiles(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + 127) / 128); }
 
 // Where what a call keeps lies in its workspace.
 struct Layout {
   int64_t rows, padded;  // rows of the window, and up to a multiple of 256
   int64_t width;         // of packed rows, in numbers
+  int64_t row;           // bytes from a packed row to the next
+  int form;              // of the products
   int planes;
   bool direct;           // the head is read where it is
   int64_t piece;         // tokens of a piece
-  int slices;            // of a piece, in the hidden states' gradient
+  int max_slices;        // of a piece's tokens, in the hidden states' gradient
   int64_t parts;
-  int64_t count, src, target, lse, mul, exp, tops, at_target, part, H, H2, W, G, dh, bytes;
+  int64_t counts, count, src, target, lse, mul, exp, tops, at_target, part, H, H2, W, G, dh, bytes;
 };
 
+// The products read a head in its place when its rows are whole steps and tiles
+// of vectors.
 bool head_direct(const epic_rows_desc* head) {
-  if (head->dtype == EPIC_F32) return false;
-  return head->vocab % 64 == 0 && head->rows % 64 == 0 && head->row_stride % 8 == 0 && head->row_stride < (1 << 21) &&
+  const int per = 16 / elem_size(head->dtype);
+  return head->vocab % 64 == 0 && head->rows % 64 == 0 && head->row_stride % per == 0 && head->row_stride < (1 << 20) &&
          ((uintptr_t)head->data & 15) == 0;
+}
+
+// Losses of few float32 rows multiply it as it is: reading the head for its
+// largest magnitude and writing it out in two parts takes longer than the slower
+// products (32768 tokens of width 2048: 64 rows 91 us, in two parts 274; 512 rows
+// 500 and 416).
+int form_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool backward) {
+  if (hidden->dtype == EPIC_F32)
+    return !backward && (int64_t)hidden->batch * hidden->rows <= 256 && head_direct(head) ? kFormF32 : kFormSplit;
+  return hidden->dtype == EPIC_F16 ? kFormF16 : kFormBf16;
 }
 
 Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool backward) {
@@ -788,22 +1064,26 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.rows = (int64_t)hidden->batch * hidden->rows;
   l.padded = up(l.rows, 256);
   l.width = up(hidden->vocab, 64);
-  l.planes = hidden->dtype == EPIC_F32 ? 2 : 1;
-  l.direct = head_direct(head);
+  l.form = form_of(hidden, head, backward);
+  l.planes = l.form == kFormSplit ? 2 : 1;
+  const int64_t es = l.form == kFormF32 ? 4 : 2;
+  l.direct = l.form != kFormSplit && head_direct(head);
   l.piece = up(V, 256);
   if (backward || !l.direct) {
     int64_t most = std::max<int64_t>(4096, (1 << 26) / std::max<int64_t>(1, std::max<int64_t>(l.direct ? 0 : l.width, backward ? l.padded : 0) * l.planes) / 256 * 256);
     const int64_t pieces = (V + most - 1) / most;
     l.piece = up((V + pieces - 1) / pieces, 256);
   }
-  l.parts = up(V, 64) / 64;
+  l.parts = up(V, 128) / 128;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t p = at;
     at += up(bytes, 256);
     return p;
   };
-  l.slices = 1;
+  // slices of the hidden states' gradient: 128 MiB of them, or one
+  l.max_slices = l.piece < 2048 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, (1 << 25) / std::max<int64_t>(1, l.padded * l.width)));
+  l.counts = take((l.padded + 63) / 64 * 8);
   l.count = take(8);
   l.src = take(4 * l.padded);
   l.target = take(4 * l.padded);
@@ -812,15 +1092,16 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.exp = take(4 * l.padded);
   l.tops = take(8 * kTopParts);
   l.at_target = take(4 * l.padded);
-  l.H = take(2 * l.planes * l.padded * l.width);
-  if (!l.direct) l.W = take(2 * l.planes * l.piece * l.width);
+  l.row = es * l.width;
+  l.H = take(l.planes * l.padded * l.row);
+  if (!l.direct) l.W = take(l.planes * l.piece * l.row);
   if (!backward) {
     l.part = take(8 * l.padded * l.parts);
   } else {
-    if (hidden->dtype != EPIC_BF16) l.H2 = take(2 * l.planes * l.padded * l.width);
+    if (l.form == kFormF16 || l.form == kFormSplit) l.H2 = take(l.planes * l.padded * l.row);
     else l.H2 = l.H;
     l.G = take(2 * l.planes * l.padded * l.piece);
-    l.dh = take(4 * l.slices * l.padded * l.width);
+    l.dh = take(4 * l.max_slices * l.padded * l.width);
   }
   l.bytes = at;
   return l;
@@ -852,32 +1133,62 @@ struct Call {
   hipStream_t stream;
 };
 
-template <int DT>
-epic_status pack_head(const Call& c, int v0, int count) {
-  PackArgs p{(const char*)c.head->data, c.head->row_stride * kSize<DT>, c.head->rows, c.head->vocab, v0, count,
-             const_cast<char*>(c.a.W.data), c.a.W.stride, c.a.W.plane, c.a.tops, {c.a.top_parts[0], c.a.top_parts[1]}};
-  hipLaunchKernelGGL(pack_kernel<DT>, dim3(std::min(2048, (count + 3) / 4)), dim3(256), 0, c.stream, p);
-  return EPIC_OK;
+template <int FORM>
+PackArgs pack_args(const Call& c, int v0) {
+  return {(const char*)c.head->data, c.head->row_stride * kSize<kDtype<FORM>>, c.head->rows, c.head->vocab, v0,
+          (int)up(std::min<int64_t>(c.head->rows - v0, c.l.piece), 64), const_cast<char*>(c.a.W.data), c.a.W.stride, c.a.W.plane,
+          (int)c.l.width, c.a.tops, {c.a.top_parts[0], c.a.top_parts[1]}};
 }
+inline int pack_groups(const PackArgs& p) { return std::min(2048, (p.count + 3) / 4); }
 
-template <int DT, int MODE>
+template <int FORM, int MODE>
 void gather(Call& c) {
   c.g.per = (int)std::max<int64_t>(4, up((c.l.rows + 4095) / 4096, 4));
-  if constexpr (DT == EPIC_F32 && MODE != kQuantize) {
-    TopArgs t{c.g, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
-    hipLaunchKernelGGL(top_kernel, dim3(c.g.top_parts[0] + c.g.top_parts[1]), dim3(256), 0, c.stream, t);
+  const int groups = (int)std::max<int64_t>(1, (c.l.rows + c.g.per - 1) / c.g.per);
+  PackArgs p{};
+  int more = 0;
+  if (c.l.rows <= 1024)
+    c.g.counts = nullptr;
+  else
+    hipLaunchKernelGGL(count_kernel, dim3((int)((c.l.rows + 255) / 256)), dim3(256), 0, c.stream, c.g);
+  if constexpr (MODE != kQuantize) {
+    if (FORM == kFormSplit) {
+      TopArgs t{c.g, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
+      hipLaunchKernelGGL(top_kernel, dim3(c.g.top_parts[0] + c.g.top_parts[1]), dim3(256), 0, c.stream, t);
+    }
+    if (!c.l.direct) {
+      p = pack_args<FORM>(c, 0);
+      more = pack_groups(p);
+    }
   }
-  hipLaunchKernelGGL((gather_kernel<DT, MODE>), dim3((int)std::max<int64_t>(1, (c.l.rows + c.g.per - 1) / c.g.per)), dim3(kGather), 0, c.stream, c.g);
+  hipLaunchKernelGGL((gather_kernel<FORM, MODE>), dim3(groups + more), dim3(kGather), 0, c.stream, c.g, p, groups);
+}
+
+// The head's piece from token v0 on.
+template <int FORM>
+void piece(Call& c, const char* whole, int v0) {
+  c.a.v0 = v0;
+  c.a.v1 = (int)std::min<int64_t>(c.a.V, v0 + c.l.piece);
+  c.a.last = c.a.v1 == c.a.V;
+  c.a.add = v0 > 0;
+  if (c.l.direct) {
+    c.a.W.data = whole + v0 * c.a.W.stride;
+  } else if (v0 > 0) {
+    const PackArgs p = pack_args<FORM>(c, v0);
+    hipLaunchKernelGGL(pack_kernel<FORM>, dim3(pack_groups(p)), dim3(256), 0, c.stream, p);
+  }
 }
 
 // What both passes set up: operands, rows that count, the head's pieces.
-template <int DT>
+template <int FORM>
 void set_up(Call& c, char* ws) {
   const Layout& l = c.l;
+  constexpr int64_t es = kPacked<FORM>;
   Kept kept{(int32_t*)(ws + l.count), (int32_t*)(ws + l.src), (int32_t*)(ws + l.target), (float*)(ws + l.lse), (float*)(ws + l.mul),
             (int32_t*)(ws + l.exp)};
-  const int64_t stride = 2 * l.width, plane = l.padded * stride;
+  const int64_t stride = l.row, plane = l.padded * stride;
   c.g.kept = c.a.kept = kept;
+  c.g.counts = (int2*)(ws + l.counts);
   c.g.out = ws + l.H;
   c.g.out2 = ws + l.H2;
   c.g.stride = stride;
@@ -888,12 +1199,11 @@ void set_up(Call& c, char* ws) {
   c.a.H = {ws + l.H, stride, plane};
   c.a.H2 = {ws + l.H2, stride, plane};
   if (l.direct)
-    c.a.W = {(const char*)c.head->data, c.head->row_stride * 2, 0};
+    c.a.W = {(const char*)c.head->data, c.head->row_stride * es, 0};
   else
     c.a.W = {ws + l.W, stride, l.piece * stride};
-  c.a.G = {ws + l.G, 2 * l.piece, l.padded * l.piece * 2};
-  c.a.steps = (int)(l.width / 64);
-  c.a.planes = l.planes;
+  c.a.G = {ws + l.G, 2 * l.piece, 2 * l.padded * l.piece};
+  c.a.steps = (int)(l.width * es / 128);
   c.a.pairs = l.planes == 2 ? kThreePairs : kOnePair;
   c.a.V = c.head->rows;
   c.a.d = c.head->vocab;
@@ -901,83 +1211,48 @@ void set_up(Call& c, char* ws) {
   c.a.part = (float2*)(ws + l.part);
   c.a.dh = (float*)(ws + l.dh);
   c.a.dh_slice = l.padded * l.width;
-  c.a.slices = l.slices;
+  c.a.max_slices = l.max_slices;
+  c.a.piece = (int)l.piece;
+  c.a.width = c.g.width = (int)l.width;
+  c.a.parts = l.parts;
   c.a.rows = c.hidden->rows;
 }
 
-template <int DT, class T>
-epic_status losses(Call& c, float* loss, float* lse) {
-  constexpr bool kSplit = DT == EPIC_F32;
-  gather<DT, kForward>(c);
-  const int V = c.a.V;
-  c.a.parts = (V + T::BN - 1) / T::BN;
-  const Operand whole = c.a.W;
-  for (int v0 = 0; v0 < V; v0 += (int)c.l.piece) {
-    c.a.v0 = v0;
-    c.a.v1 = (int)std::min<int64_t>(V, v0 + c.l.piece);
-    if (c.l.direct)
-      c.a.W.data = whole.data + v0 * whole.stride;
-    else
-      pack_head<DT>(c, v0, (int)up(c.a.v1 - v0, 64));
-    const int64_t tiles = (c.l.rows + T::BM - 1) / T::BM * ((c.a.v1 - v0 + T::BN - 1) / T::BN);
-    const epic_status st = launch_tiles<T>(lse_kernel<T, kSplit>, c.a, tiles, c.stream);
-    if (st != EPIC_OK) return st;
+template <int FORM>
+void losses(Call& c, char* ws, float* loss, float* lse) {
+  set_up<FORM>(c, ws);
+  gather<FORM, kForward>(c);
+  const char* whole = c.a.W.data;
+  for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
+    piece<FORM>(c, whole, (int)v0);
+    launch_product(lse_kernel<FORM>, c.a, most_tiles(c.l.rows, c.a.v1 - c.a.v0), c.stream);
   }
-  c.a.first = 0;
-  hipLaunchKernelGGL(loss_kernel, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a, loss, lse);
-  return EPIC_OK;
+  hipLaunchKernelGGL(loss_kernel<FORM>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a, loss, lse);
 }
 
-template <int DT, class T, class TH, class TW>
-epic_status gradients(Call& c, const epic_rows_desc* gh, const epic_rows_desc* gw) {
-  constexpr bool kSplit = DT == EPIC_F32;
-  gather<DT, kBackward>(c);
-  const int V = c.a.V, d = c.a.d;
-  const Operand whole = c.a.W;
-  for (int v0 = 0; v0 < V; v0 += (int)c.l.piece) {
-    c.a.v0 = v0;
-    c.a.v1 = (int)std::min<int64_t>(V, v0 + c.l.piece);
-    const int count = c.a.v1 - v0;
-    if (c.l.direct)
-      c.a.W.data = whole.data + v0 * whole.stride;
-    else
-      pack_head<DT>(c, v0, (int)up(count, 64));
-    epic_status st = launch_tiles<T>(excess_kernel<T, kSplit>, c.a, (c.l.rows + T::BM - 1) / T::BM * ((count + T::BN - 1) / T::BN), c.stream);
-    if (st == EPIC_OK && gh) {
-      c.a.add = v0 > 0;
-      st = launch_tiles<TH>(grad_hidden_kernel<TH, kSplit>, c.a,
-                            (c.l.rows + TH::BM - 1) / TH::BM * ((d + TH::BN - 1) / TH::BN) * c.a.slices, c.stream);
-    }
-    if (st == EPIC_OK && gw) {
-      c.a.grad_head = (char*)gw->data;
-      c.a.grad_row = gw->row_stride * kSize<DT>;
-      st = launch_tiles<TW>(grad_head_kernel<TW, kSplit, DT>, c.a,
-                            (int64_t)((count + TW::BM - 1) / TW::BM) * ((d + TW::BN - 1) / TW::BN), c.stream);
-    }
-    if (st != EPIC_OK) return st;
-  }
+template <int FORM>
+void gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc* gw) {
+  set_up<FORM>(c, ws);
   if (gh && c.l.rows > 0) {
-    c.a.first = 0;
-    hipLaunchKernelGGL(scatter_kernel<DT>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a, (char*)gh->data,
-                       gh->seq_stride * kSize<DT>, gh->row_stride * kSize<DT>);
+    c.a.grad_hidden = (char*)gh->data;
+    c.a.gh_seq = gh->seq_stride * kSize<kDtype<FORM>>;
+    c.a.gh_row = gh->row_stride * kSize<kDtype<FORM>>;
   }
-  return EPIC_OK;
-}
-
-template <int DT>
-epic_status run_losses(Call& c, char* ws, float* loss, float* lse) {
-  constexpr int K = DT == EPIC_BF16 ? kBf16 : kF16;
-  set_up<DT>(c, ws);
-  if (c.l.rows * c.a.V <= 256 * 256 * 256) return losses<DT, Small<K>>(c, loss, lse);
-  return losses<DT, Large<K>>(c, loss, lse);
-}
-template <int DT>
-epic_status run_gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc* gw) {
-  constexpr int K = DT == EPIC_BF16 ? kBf16 : kF16;
-  set_up<DT>(c, ws);
-  if (c.l.rows * c.a.V <= 256 * 256 * 256)
-    return gradients<DT, Small<K>, Tile<K, 64, 64, 2, 2, 4, true, false>, Tile<K, 64, 64, 2, 2, 4, false, false>>(c, gh, gw);
-  return gradients<DT, Large<K>, Tile<K, 256, 256, 2, 4, 2, true, false>, Tile<K, 256, 256, 2, 4, 2, false, false>>(c, gh, gw);
+  if (gw) {
+    c.a.grad_head = (char*)gw->data;
+    c.a.grad_row = gw->row_stride * kSize<kDtype<FORM>>;
+  }
+  gather<FORM, kBackward>(c);
+  const char* whole = c.a.W.data;
+  const int d = c.a.d;
+  for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
+    piece<FORM>(c, whole, (int)v0);
+    const int count = c.a.v1 - c.a.v0;
+    launch_product(excess_kernel<FORM>, c.a, most_tiles(c.l.rows, count), c.stream);
+    launch_product(grad_kernel<FORM>, c.a, (gh ? most_tiles(c.l.rows, d) * c.a.max_slices : 0) + (gw ? most_tiles(count, d) : 0), c.stream);
+  }
+  if (c.a.grad_hidden && c.a.max_slices > 1)
+    hipLaunchKernelGGL(scatter_kernel<FORM>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a);
 }
 
 epic_status head_loss(bool backward, const epic_rows_desc* hidden, const int32_t* d_seqs, int32_t n, const int32_t* d_start,
@@ -1030,12 +1305,14 @@ epic_status head_loss(bool backward, const epic_rows_desc* hidden, const int32_t
     c.g.grad_row = grad_hidden->row_stride * es;
   }
   char* ws = (char*)d_workspace;
-  switch (hidden->dtype) {
-    case EPIC_F32: st = backward ? run_gradients<EPIC_F32>(c, ws, grad_hidden, grad_head) : run_losses<EPIC_F32>(c, ws, d_loss, d_lse); break;
-    case EPIC_F16: st = backward ? run_gradients<EPIC_F16>(c, ws, grad_hidden, grad_head) : run_losses<EPIC_F16>(c, ws, d_loss, d_lse); break;
-    default: st = backward ? run_gradients<EPIC_BF16>(c, ws, grad_hidden, grad_head) : run_losses<EPIC_BF16>(c, ws, d_loss, d_lse); break;
+#define EPIC_HEAD(FORM) backward ? gradients<FORM>(c, ws, grad_hidden, grad_head) : losses<FORM>(c, ws, d_loss, d_lse)
+  switch (l.form) {
+    case kFormF32: losses<kFormF32>(c, ws, d_loss, d_lse); break;
+    case kFormSplit: EPIC_HEAD(kFormSplit); break;
+    case kFormF16: EPIC_HEAD(kFormF16); break;
+    default: EPIC_HEAD(kFormBf16);
   }
-  if (st != EPIC_OK) return st;
+#undef EPIC_HEAD
   return hipGetLastError() == hipSuccess ? EPIC_OK : EPIC_ERR_HIP;
 }
 
@@ -1047,7 +1324,7 @@ void run_quantize(const epic_rows_desc* x, int8_t* q, int64_t stride, float* sca
 }
 
 struct LogitsLayout {
-  int64_t rows, padded, stride, count, src, scale, H, bytes;
+  int64_t rows, padded, stride, counts, count, src, scale, H, bytes;
 };
 LogitsLayout logits_layout(const epic_rows_desc* hidden) {
   LogitsLayout l{};
@@ -1058,18 +1335,9 @@ LogitsLayout logits_layout(const epic_rows_desc* hidden) {
   l.src = 256;
   l.scale = l.src + 4 * l.padded;
   l.H = l.scale + 4 * l.padded;
-  l.bytes = l.H + l.padded * l.stride;
+  l.counts = l.H + l.padded * l.stride;
+  l.bytes = l.counts + up((l.padded + 63) / 64 * 8, 256);
   return l;
-}
-
-template <class T>
-epic_status run_logits(const HeadArgs& a, int dtype, int64_t rows, hipStream_t stream) {
-  const int64_t tiles = (rows + T::BM - 1) / T::BM * ((a.V + T::BN - 1) / T::BN);
-  switch (dtype) {
-    case EPIC_F32: return launch_tiles<T>(logits_kernel<T, EPIC_F32>, a, tiles, stream);
-    case EPIC_F16: return launch_tiles<T>(logits_kernel<T, EPIC_F16>, a, tiles, stream);
-    default: return launch_tiles<T>(logits_kernel<T, EPIC_BF16>, a, tiles, stream);
-  }
 }
 
 }  // namespace epic_rows
@@ -1128,10 +1396,11 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
   c.g.out = ws + l.H;
   c.g.stride = l.stride;
   c.g.scale = (float*)(ws + l.scale);
+  c.g.counts = (int2*)(ws + l.counts);
   switch (hidden->dtype) {
-    case EPIC_F32: gather<EPIC_F32, kQuantize>(c); break;
-    case EPIC_F16: gather<EPIC_F16, kQuantize>(c); break;
-    default: gather<EPIC_BF16, kQuantize>(c); break;
+    case EPIC_F32: gather<kFormF32, kQuantize>(c); break;
+    case EPIC_F16: gather<kFormF16, kQuantize>(c); break;
+    default: gather<kFormBf16, kQuantize>(c); break;
   }
   HeadArgs& a = c.a;
   a.kept = c.g.kept;
@@ -1145,11 +1414,12 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
   a.seq_stride = logits->seq_stride * eo;
   a.row_stride = logits->row_stride * eo;
   a.rows = hidden->rows;
-  if (l.rows * a.V <= 256 * 256 * 256)
-    st = run_logits<Small<kI8>>(a, logits->dtype, l.rows, stream);
-  else
-    st = run_logits<Large<kI8>>(a, logits->dtype, l.rows, stream);
-  if (st != EPIC_OK) return st;
+  const int64_t tiles = most_tiles(l.rows, a.V);
+  switch (logits->dtype) {
+    case EPIC_F32: launch_product(logits_kernel<EPIC_F32>, a, tiles, stream); break;
+    case EPIC_F16: launch_product(logits_kernel<EPIC_F16>, a, tiles, stream); break;
+    default: launch_product(logits_kernel<EPIC_BF16>, a, tiles, stream); break;
+  }
   return hipGetLastError() == hipSuccess ? EPIC_OK : EPIC_ERR_HIP;
 }
 
