@@ -15,6 +15,7 @@ template <int FORM>
 constexpr int kKind = FORM == kFormBf16 ? kBf16 : FORM == kFormF32 ? kF32 : kF16;
 template <int FORM>
 constexpr int kPairs = FORM == kFormSplit ? 3 : 1;
+constexpr uint32_t kThreePairs = 0x014;  // planes (0, 1), (1, 0), (0, 0): small products first
 template <int FORM>
 constexpr int kPacked = FORM == kFormF32 ? 4 : 2;  // bytes of a number that products read
 template <int FORM>
@@ -46,8 +47,9 @@ struct GatherArgs {
   int64_t grad_seq, grad_row;
   Kept kept;
   char* out;         // packed rows
-  char* out2;        // 16-bit numbers with the rows' powers of two, for the product over rows
-  int64_t stride, plane;  // bytes
+  int64_t stride, plane;    // bytes
+  char* out2;        // with the rows' powers of two, for the product over rows
+  int64_t stride2, plane2;
   int width;         // of packed rows, in numbers
   float* scale;      // 8 bits: the rows' scales
   const float* tops; // 32 bits: largest magnitudes of hidden states and head, in parts
@@ -235,10 +237,10 @@ EPIC_DEV void quantize_row(const char* row, int d, int8_t* out, int stride, floa
   }
 }
 
-// A row to packed 16-bit numbers, multiplied with 2^e; with a second place also
-// with 2^e2.
-template <int FORM, bool TWO>
-EPIC_DEV void pack_row(const char* row, int d, char* out, char* out2, int64_t plane, int width, int e, int e2, int lane) {
+// A row to packed numbers as FORM has them, multiplied with 2^e; with TWO also as
+// FORM2 has them, multiplied with 2^(e + e2).
+template <int FORM, int FORM2, bool TWO>
+EPIC_DEV void pack_row(const char* row, int d, int width, char* out, int64_t plane, int e, char* out2, int64_t plane2, int e2, int lane) {
   constexpr int N = 4;  // loads ahead
   for (int t0 = 0; t0 < width; t0 += 512 * N) {
     float x[N][8];
@@ -255,8 +257,8 @@ EPIC_DEV void pack_row(const char* row, int d, char* out, char* out2, int64_t pl
       store8<FORM>(out, plane, t, x[j]);
       if constexpr (TWO) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[j][k] = __builtin_amdgcn_ldexpf(x[j][k], e2);
-        store8<FORM>(out2, plane, t, x[j]);
+        for (int k = 0; k < 8; ++k) x[j][k] = __builtin_amdgcn_ldexpf(x[j][k], FORM == kFormSplit ? e2 : e + e2);
+        store8<FORM2>(out2, plane2, t, x[j]);
       }
     }
   }
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(256) count_kernel(GatherArgs a) {
 // 64 (the gradients' products sum over them).  Every workgroup counts the rows
 // before its own itself, so that one launch does it for up to 1024 rows; of more it
 // adds up count_kernel's numbers of 64 rows each.
-template <int FORM, int MODE>
+template <int FIRST, int FORM, int MODE>
 EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather / 64], int (&lds_own)[64], float (&lds_f)[kGather / 64]) {
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int total = a.batch * a.rows, first = group * a.per, last = min(total, first + a.per);
@@ -373,8 +375,8 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
           }
         }
         // a row that adds nothing has no numbers
-        pack_row<FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.out + at * a.stride, a.out2 + at * a.stride, a.plane,
-                              a.width, h_exp, shift, lane);
+        pack_row<FIRST, FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.width, a.out + at * a.stride, a.plane, h_exp,
+                                        a.out2 + at * a.stride2, a.plane2, shift, lane);
       }
     }
   }
@@ -383,15 +385,11 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
     if constexpr (kWeights)
       if (tid == 0) a.kept.count[1] = top_exp == -1000 ? 0 : top_exp;
     if constexpr (MODE == kBackward) {
-      const int end = (before + 63) / 64 * 64, vecs = (int)(a.stride / 16);
+      const int end = (before + 63) / 64 * 64, vecs = (int)(a.stride2 / 16);
       for (int i = tid; i < (end - before) * vecs; i += kGather) {
-        const int64_t at = (int64_t)before * a.stride + (int64_t)i * 16;
-        *(uint4*)(a.out + at) = make_uint4(0, 0, 0, 0);
-        if constexpr (kWeights) *(uint4*)(a.out2 + at) = make_uint4(0, 0, 0, 0);
-        if constexpr (FORM == kFormSplit) {
-          *(uint4*)(a.out + a.plane + at) = make_uint4(0, 0, 0, 0);
-          *(uint4*)(a.out2 + a.plane + at) = make_uint4(0, 0, 0, 0);
-        }
+        char* to = a.out2 + (int64_t)before * a.stride2 + (int64_t)i * 16;
+        *(uint4*)to = make_uint4(0, 0, 0, 0);
+        if constexpr (FORM == kFormSplit) *(uint4*)(to + a.plane2) = make_uint4(0, 0, 0, 0);
       }
     }
   }
@@ -455,8 +453,8 @@ EPIC_DEV void pack_rows(const PackArgs& a, int group, int groups, float* lds) {
   int e_head = 0;
   if constexpr (FORM == kFormSplit) e_head = scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
   for (int i = group * 4 + wave; i < a.count; i += groups * 4)
-    pack_row<FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.out + i * a.stride, nullptr, a.plane,
-                        a.width, e_head, 0, lane);
+    pack_row<FORM, FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.width, a.out + i * a.stride, a.plane, e_head,
+                                nullptr, 0, 0, lane);
 }
 template <int FORM>
 __global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
@@ -466,13 +464,13 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
 
 // The rows that count by the first `groups` workgroups, and by the others the
 // head's first piece where it has to be packed.
-template <int FORM, int MODE>
+template <int FIRST, int FORM, int MODE>
 __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a, PackArgs p, int groups) {
   __shared__ int lds_n[kGather / 64];
   __shared__ int lds_own[64];
   __shared__ float lds_f[kGather / 64];
   if ((int)blockIdx.x < groups)
-    gather_rows<FORM, MODE>(a, (int)blockIdx.x, lds_n, lds_own, lds_f);
+    gather_rows<FIRST, FORM, MODE>(a, (int)blockIdx.x, lds_n, lds_own, lds_f);
   else if constexpr (MODE != kQuantize)
     pack_rows<FORM>(p, (int)blockIdx.x - groups, (int)gridDim.x - groups, lds_f);
 }
@@ -489,12 +487,12 @@ __global__ void __launch_bounds__(256) quantize_kernel(const char* data, int64_t
 
 // ------------------------------------------------------------- products
 struct HeadArgs {
-  Operand H, W;      // rows that count [N, d], (a piece of) the head [v, d]
+  Operand H, W;      // rows that count [N, d], (a piece of) the head [v, d], for the logits
+  Operand H2, W2;    // and for the gradients
   Kept kept;
   int steps;         // of d
   int piece;         // tokens of a whole piece
   int width;         // d up to a multiple of 64
-  uint32_t pairs;
   int v0, v1;        // tokens of the piece
   int V, d;
   // losses
@@ -505,7 +503,6 @@ struct HeadArgs {
   int top_parts[2];
   // gradients
   Operand G;         // (p - y) of the piece [N, v] in 16 bits
-  Operand H2;
   float* dh;         // [slices][rows][d] float32
   int64_t dh_slice;
   int max_slices, add, last;  // last: the piece after which gradients are whole
@@ -536,11 +533,11 @@ constexpr int kProductThreads = 512, kProductLds = 131072, kCus = 256;
 EPIC_DEV int ceil_div(int a, int b) { return (a + b - 1) / b; }
 // 0 large, 1 mid, 2 few: of a result of m x n sums, `copies` times.  The rounds
 // that the CUs take, by what a round of each size costs.
+EPIC_DEV int tile_cost(int size) { return size == 0 ? 20 : size == 1 ? 9 : 6; }
 template <int KIND>
 EPIC_DEV int tile_size(int m, int n, int copies = 1) {
-  const int c0 = ceil_div(ceil_div(m, 256) * ceil_div(n, 256) * copies, kCus) * (KIND == kF32 ? 32 : 20);
-  const int c1 = ceil_div(ceil_div(m, 128) * ceil_div(n, 128) * copies, kCus) * 9;
-  const int c2 = ceil_div(ceil_div(m, 64) * ceil_div(n, 128) * copies, kCus) * (KIND == kF32 ? 5 : 6);
+  const auto rounds = [&](int rows, int cols) { return ((int64_t)ceil_div(m, rows) * ceil_div(n, cols) * copies + kCus - 1) / kCus; };
+  const int64_t c0 = rounds(256, 256) * (KIND == kF32 ? 32 : 20), c1 = rounds(128, 128) * 9, c2 = rounds(64, 128) * (KIND == kF32 ? 5 : 6);
   return c2 < c1 && c2 < c0 ? 2 : c1 < c0 ? 1 : 0;
 }
 template <class S, class F>
@@ -579,7 +576,7 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
       [&](int id) {
         int tm, tn;
         place(id, tm, tn);
-        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, a.pairs);
+        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FORM> == 3 ? kThreePairs : 0);
       },
       [&](int id, int k) {
         int tm, tn;
@@ -679,18 +676,18 @@ __global__ void __launch_bounds__(256) loss_kernel(HeadArgs a, float* loss, floa
 // weights are in [1/2, 1): 2^-24 of p = 1 is a normal number.  Numbers of rows past
 // the last, of rows without a token (which have hidden states 0 and weight 0) and
 // of columns past the vocabulary are 0: the products that follow sum over them.
-template <int FORM, class T>
+template <int FIRST, int FORM, class T>
 EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* smem, int (&target)[2][256], float2 (&scale)[2][256]) {
   constexpr float kScale = kScaled<FORM> ? 16384.f : 1.f;
   const int m = ceil_div(count, T::BM), n = ceil_div(a.v1 - a.v0, T::BN);
   const float c = by * kLog2e;
   auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
-  every_tile<kPairs<FORM>>(
+  every_tile<kPairs<FIRST>>(
       t, smem, [&](int i) { return dealt(i, m * n); },
       [&](int id) {
         int tm, tn;
         place(id, tm, tn);
-        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, a.pairs);
+        t.template start<kPairs<FIRST>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FIRST> == 3 ? kThreePairs : 0);
       },
       [&](int id, int k) {
         int tm, tn;
@@ -727,11 +724,13 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
             for (int f = 0; f < 4 * T::F; ++f)
               g[f] = x.y * __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j + f / 4][f & 3], c, -x.x));
             const int c0 = T::col(j, lane);
-            if (some) {
+            if (some && (unsigned)(y - c0) < (unsigned)(4 * T::F)) {  // 1 - p without what p = 1 rounds away
+              float l = 0.f;
 #pragma unroll
-              for (int f = 0; f < 4 * T::F; ++f)
-                if (c0 + f == y)  // 1 - p without what p = 1 rounds away
-                  g[f] = a.kept.mul[at] * kScale * expm1f(t.acc[i][j + f / 4][f & 3] * by - a.kept.lse[at]);
+              for (int f = 0; f < 4 * T::F; ++f) l = c0 + f == y ? t.acc[i][j + f / 4][f & 3] : l;
+              const float own = a.kept.mul[at] * kScale * expm1f(l * by - a.kept.lse[at]);
+#pragma unroll
+              for (int f = 0; f < 4 * T::F; ++f) g[f] = c0 + f == y ? own : g[f];
             }
             if (cols < T::BN || (tm + 1) * T::BM > count) {
 #pragma unroll
@@ -746,15 +745,15 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
         }
       });
 }
-template <int FORM>
+template <int FIRST, int FORM>
 __global__ void __launch_bounds__(kProductThreads) excess_kernel(HeadArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[kProductLds];
   __shared__ float lds_top[kProductThreads / 64];
   __shared__ int target[2][256];
   __shared__ float2 scale[2][256];  // lse in powers of two, and what 2^(l - lse) is multiplied with
   const int count = *a.kept.count;
-  const float by = unscale<FORM>(a, lds_top);
-  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { excess_tiles<FORM>(a, t, count, by, smem, target, scale); });
+  const float by = unscale<FIRST>(a, lds_top);
+  with_size<Sizes<kKind<FIRST>, true, true>>(tile_size<kKind<FIRST>>(count, a.piece), [&](auto& t) { excess_tiles<FIRST, FORM>(a, t, count, by, smem, target, scale); });
 }
 
 // ---- The two products with G, in one launch: the hidden states' gradient G W
@@ -779,15 +778,16 @@ EPIC_DEV Split split_of(const HeadArgs& a, int count) {
   s.n_h = ceil_div(a.d, hn);
   s.m_w = ceil_div(a.v1 - a.v0, wm);
   s.n_w = ceil_div(a.d, wn);
-  // in steps of a 64 x 128 tile; a tile's start and end are worth some
-  const int k_h = ceil_div(a.piece, 64), k_w = ceil_div(count, 64) + 8, area_h = hm * hn / 8192, area_w = wm * wn / 8192;
-  const int64_t all = (a.grad_hidden ? (int64_t)s.m_h * s.n_h * k_h * area_h : 0) +
-                      (a.grad_head ? (int64_t)ceil_div(a.piece, wm) * s.n_w * k_w * area_w : 0);
+  // by what a step of a tile costs; a tile's start and end are worth some steps
+  const int k_h = ceil_div(a.piece, 64), k_w = ceil_div(count, 64) + 8, cost_h = tile_cost(s.size_h), cost_w = tile_cost(s.size_w);
+  const int64_t all = (a.grad_hidden ? (int64_t)s.m_h * s.n_h * k_h * cost_h : 0) +
+                      (a.grad_head ? (int64_t)ceil_div(a.piece, wm) * s.n_w * k_w * cost_w : 0);
+  // Slices of no more than 4/5 of what each CU has to do (2867 rows of 32768 tokens,
+  // width 2048, both passes: 1.05 ms; of 4/3 of it 1.18, of 2/5 1.07), and of at
+  // least 1024 tokens.
   s.slices = 1;
-  while (2 * s.slices <= a.max_slices && k_h >= 32 * s.slices &&
-         (int64_t)k_h * area_h * 4 * kCus > 3 * all * s.slices)
-    s.slices *= 2;
-  s.lead = (int)(((int64_t)k_h / s.slices + 8) * area_h / (k_w * area_w));
+  while (2 * s.slices <= a.max_slices && k_h >= 16 * s.slices && (int64_t)k_h * cost_h * 5 * kCus > 4 * all * s.slices) s.slices *= 2;
+  s.lead = (int)(((int64_t)k_h / s.slices + 8) * cost_h / (k_w * cost_w));
   return s;
 }
 
@@ -808,7 +808,7 @@ EPIC_DEV void grad_hidden_tiles(const HeadArgs& a, T& t, const Split& s, int cou
         int tm, tn;
         const int slice = place(id, tm, tn);
         const int k0 = (int)((int64_t)all * slice / s.slices), k1 = (int)((int64_t)all * (slice + 1) / s.slices);
-        t.template start<P>(a.G, a.W, tm * T::BM, tn * T::BN, m * T::BM, dp, k0, k1 - k0, a.pairs);
+        t.template start<P>(a.G, a.W2, tm * T::BM, tn * T::BN, m * T::BM, dp, k0, k1 - k0, P == 3 ? kThreePairs : 0);
       },
       [](int, int) {},
       [&](int id, int) {
@@ -868,7 +868,7 @@ EPIC_DEV void grad_head_tiles(const HeadArgs& a, T& t, const Split& s, int count
       [&](int id) {
         int tm, tn;
         tile_of(id, m, n, tm, tn);
-        t.template start<P>(a.G, a.H2, tm * T::BM, tn * T::BN, m * T::BM, a.width, 0, ceil_div(count, 64), a.pairs);
+        t.template start<P>(a.G, a.H2, tm * T::BM, tn * T::BN, m * T::BM, a.width, 0, ceil_div(count, 64), P == 3 ? kThreePairs : 0);
       },
       [](int, int) {},
       [&](int id, int) {
@@ -1030,10 +1030,9 @@ inline int64_t most_tiles(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + 1
 struct Layout {
   int64_t rows, padded;  // rows of the window, and up to a multiple of 256
   int64_t width;         // of packed rows, in numbers
-  int64_t row;           // bytes from a packed row to the next
-  int form;              // of the products
-  int planes;
-  bool direct;           // the head is read where it is
+  int first, form;       // of the logits' product, of the gradients' (the same but for few float32 rows)
+  bool direct;           // the head is read where it is, for the logits,
+  bool packed;           // or (and) written out
   int64_t piece;         // tokens of a piece
   int max_slices;        // of a piece's tokens, in the hidden states' gradient
   int64_t parts;
@@ -1048,14 +1047,13 @@ bool head_direct(const epic_rows_desc* head) {
          ((uintptr_t)head->data & 15) == 0;
 }
 
-// Losses of few float32 rows multiply it as it is: reading the head for its
-// largest magnitude and writing it out in two parts takes longer than the slower
-// products (32768 tokens of width 2048: 64 rows 91 us, in two parts 274; 512 rows
-// 500 and 416).
-int form_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool backward) {
-  if (hidden->dtype == EPIC_F32)
-    return !backward && (int64_t)hidden->batch * hidden->rows <= 256 && head_direct(head) ? kFormF32 : kFormSplit;
-  return hidden->dtype == EPIC_F16 ? kFormF16 : kFormBf16;
+// Logits of few float32 rows multiply numbers as they are: reading the head for
+// its largest magnitude and writing it out in two parts takes longer than the
+// slower products (losses, 32768 tokens of width 2048: 64 rows 91 us, in two parts
+// 274; 512 rows 500 and 416).  Both passes do so: exp(l - lse) is to have the
+// errors of one l.
+bool as_it_is(const epic_rows_desc* hidden, const epic_rows_desc* head) {
+  return hidden->dtype == EPIC_F32 && (int64_t)hidden->batch * hidden->rows <= 128 && head_direct(head);
 }
 
 Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool backward) {
@@ -1064,13 +1062,17 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.rows = (int64_t)hidden->batch * hidden->rows;
   l.padded = up(l.rows, 256);
   l.width = up(hidden->vocab, 64);
-  l.form = form_of(hidden, head, backward);
-  l.planes = l.form == kFormSplit ? 2 : 1;
-  const int64_t es = l.form == kFormF32 ? 4 : 2;
-  l.direct = l.form != kFormSplit && head_direct(head);
+  l.form = hidden->dtype == EPIC_F32 ? kFormSplit : hidden->dtype == EPIC_F16 ? kFormF16 : kFormBf16;
+  l.first = as_it_is(hidden, head) ? kFormF32 : l.form;
+  const bool split = l.form == kFormSplit;
+  l.direct = split ? l.first == kFormF32 : head_direct(head);
+  l.packed = !l.direct || (split && backward);
+  const int planes = split ? 2 : 1;
   l.piece = up(V, 256);
-  if (backward || !l.direct) {
-    int64_t most = std::max<int64_t>(4096, (1 << 26) / std::max<int64_t>(1, std::max<int64_t>(l.direct ? 0 : l.width, backward ? l.padded : 0) * l.planes) / 256 * 256);
+  if (backward || l.packed) {
+    // 128 MiB of G, 256 of the head, but not less than a launch takes to fill the CUs
+    const int64_t wide = std::max<int64_t>(l.packed ? (l.width + 1) / 2 : 0, backward ? l.padded : 0);
+    const int64_t most = std::max<int64_t>(4096, (1 << 26) / std::max<int64_t>(1, wide * planes) / 256 * 256);
     const int64_t pieces = (V + most - 1) / most;
     l.piece = up((V + pieces - 1) / pieces, 256);
   }
@@ -1092,15 +1094,14 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.exp = take(4 * l.padded);
   l.tops = take(8 * kTopParts);
   l.at_target = take(4 * l.padded);
-  l.row = es * l.width;
-  l.H = take(l.planes * l.padded * l.row);
-  if (!l.direct) l.W = take(l.planes * l.piece * l.row);
+  const int64_t whole = 2 * planes * l.width;  // bytes of a packed row in all its planes
+  l.H = take(l.padded * (l.first == kFormF32 ? 4 * l.width : whole));
+  if (l.packed) l.W = take(l.piece * whole);
   if (!backward) {
     l.part = take(8 * l.padded * l.parts);
   } else {
-    if (l.form == kFormF16 || l.form == kFormSplit) l.H2 = take(l.planes * l.padded * l.row);
-    else l.H2 = l.H;
-    l.G = take(2 * l.planes * l.padded * l.piece);
+    l.H2 = l.form == kFormBf16 ? l.H : take(l.padded * whole);
+    l.G = take(2 * planes * l.padded * l.piece);
     l.dh = take(4 * l.max_slices * l.padded * l.width);
   }
   l.bytes = at;
@@ -1122,9 +1123,6 @@ epic_status check_head(const epic_rows_desc* hidden, const epic_rows_desc* head)
   return EPIC_OK;
 }
 
-constexpr uint32_t kOnePair = 0;
-constexpr uint32_t kThreePairs = 0x014;  // (0, 1), (1, 0), (0, 0): small products first
-
 struct Call {
   const epic_rows_desc *hidden, *head;
   Layout l;
@@ -1136,12 +1134,12 @@ struct Call {
 template <int FORM>
 PackArgs pack_args(const Call& c, int v0) {
   return {(const char*)c.head->data, c.head->row_stride * kSize<kDtype<FORM>>, c.head->rows, c.head->vocab, v0,
-          (int)up(std::min<int64_t>(c.head->rows - v0, c.l.piece), 64), const_cast<char*>(c.a.W.data), c.a.W.stride, c.a.W.plane,
+          (int)up(std::min<int64_t>(c.head->rows - v0, c.l.piece), 64), const_cast<char*>(c.a.W2.data), c.a.W2.stride, c.a.W2.plane,
           (int)c.l.width, c.a.tops, {c.a.top_parts[0], c.a.top_parts[1]}};
 }
 inline int pack_groups(const PackArgs& p) { return std::min(2048, (p.count + 3) / 4); }
 
-template <int FORM, int MODE>
+template <int FIRST, int FORM, int MODE>
 void gather(Call& c) {
   c.g.per = (int)std::max<int64_t>(4, up((c.l.rows + 4095) / 4096, 4));
   const int groups = (int)std::max<int64_t>(1, (c.l.rows + c.g.per - 1) / c.g.per);
@@ -1152,27 +1150,29 @@ void gather(Call& c) {
   else
     hipLaunchKernelGGL(count_kernel, dim3((int)((c.l.rows + 255) / 256)), dim3(256), 0, c.stream, c.g);
   if constexpr (MODE != kQuantize) {
-    if (FORM == kFormSplit) {
+    if (FORM == kFormSplit && (FIRST == kFormSplit || MODE == kBackward)) {
       TopArgs t{c.g, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
       hipLaunchKernelGGL(top_kernel, dim3(c.g.top_parts[0] + c.g.top_parts[1]), dim3(256), 0, c.stream, t);
     }
-    if (!c.l.direct) {
+    if (c.l.packed) {
       p = pack_args<FORM>(c, 0);
       more = pack_groups(p);
     }
   }
-  hipLaunchKernelGGL((gather_kernel<FORM, MODE>), dim3(groups + more), dim3(kGather), 0, c.stream, c.g, p, groups);
+  hipLaunchKernelGGL((gather_kernel<FIRST, FORM, MODE>), dim3(groups + more), dim3(kGather), 0, c.stream, c.g, p, groups);
 }
 
 // The head's piece from token v0 on.
 template <int FORM>
-void piece(Call& c, const char* whole, int v0) {
+void piece(Call& c, int v0) {
   c.a.v0 = v0;
   c.a.v1 = (int)std::min<int64_t>(c.a.V, v0 + c.l.piece);
   c.a.last = c.a.v1 == c.a.V;
   c.a.add = v0 > 0;
-  if (c.l.direct) {
-    c.a.W.data = whole + v0 * c.a.W.stride;
+  const char* raw = (const char*)c.head->data + v0 * c.head->row_stride * elem_size(c.head->dtype);
+  if (c.l.direct) c.a.W.data = raw;
+  if (!c.l.packed) {
+    c.a.W2.data = raw;
   } else if (v0 > 0) {
     const PackArgs p = pack_args<FORM>(c, v0);
     hipLaunchKernelGGL(pack_kernel<FORM>, dim3(pack_groups(p)), dim3(256), 0, c.stream, p);
@@ -1180,31 +1180,30 @@ void piece(Call& c, const char* whole, int v0) {
 }
 
 // What both passes set up: operands, rows that count, the head's pieces.
-template <int FORM>
+template <int FIRST, int FORM>
 void set_up(Call& c, char* ws) {
   const Layout& l = c.l;
-  constexpr int64_t es = kPacked<FORM>;
   Kept kept{(int32_t*)(ws + l.count), (int32_t*)(ws + l.src), (int32_t*)(ws + l.target), (float*)(ws + l.lse), (float*)(ws + l.mul),
             (int32_t*)(ws + l.exp)};
-  const int64_t stride = l.row, plane = l.padded * stride;
+  const int64_t es = kPacked<FIRST>, stride = es * l.width, plane = l.padded * stride, stride2 = 2 * l.width, plane2 = l.padded * stride2;
   c.g.kept = c.a.kept = kept;
   c.g.counts = (int2*)(ws + l.counts);
   c.g.out = ws + l.H;
-  c.g.out2 = ws + l.H2;
   c.g.stride = stride;
   c.g.plane = plane;
+  c.g.out2 = ws + l.H2;
+  c.g.stride2 = stride2;
+  c.g.plane2 = plane2;
   c.g.tops = c.a.tops = (float*)(ws + l.tops);
   c.g.top_parts[0] = c.a.top_parts[0] = (int)std::min<int64_t>(kTopParts, (l.rows + 3) / 4);
   c.g.top_parts[1] = c.a.top_parts[1] = std::min(kTopParts, (c.head->rows + 3) / 4);
   c.a.H = {ws + l.H, stride, plane};
-  c.a.H2 = {ws + l.H2, stride, plane};
-  if (l.direct)
-    c.a.W = {(const char*)c.head->data, c.head->row_stride * es, 0};
-  else
-    c.a.W = {ws + l.W, stride, l.piece * stride};
+  c.a.H2 = {ws + l.H2, stride2, plane2};
+  const Operand raw{(const char*)c.head->data, c.head->row_stride * es, 0}, written{ws + l.W, stride2, l.piece * stride2};
+  c.a.W = l.direct ? raw : written;
+  c.a.W2 = l.packed ? written : raw;
   c.a.G = {ws + l.G, 2 * l.piece, 2 * l.padded * l.piece};
-  c.a.steps = (int)(l.width * es / 128);
-  c.a.pairs = l.planes == 2 ? kThreePairs : kOnePair;
+  c.a.steps = (int)(stride / 128);
   c.a.V = c.head->rows;
   c.a.d = c.head->vocab;
   c.a.at_target = (float*)(ws + l.at_target);
@@ -1218,21 +1217,21 @@ void set_up(Call& c, char* ws) {
   c.a.rows = c.hidden->rows;
 }
 
+// FORM: of the logits' product.
 template <int FORM>
 void losses(Call& c, char* ws, float* loss, float* lse) {
-  set_up<FORM>(c, ws);
-  gather<FORM, kForward>(c);
-  const char* whole = c.a.W.data;
+  set_up<FORM, FORM>(c, ws);
+  gather<FORM, FORM, kForward>(c);
   for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
-    piece<FORM>(c, whole, (int)v0);
+    piece<FORM>(c, (int)v0);
     launch_product(lse_kernel<FORM>, c.a, most_tiles(c.l.rows, c.a.v1 - c.a.v0), c.stream);
   }
   hipLaunchKernelGGL(loss_kernel<FORM>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a, loss, lse);
 }
 
-template <int FORM>
+template <int FIRST, int FORM>
 void gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc* gw) {
-  set_up<FORM>(c, ws);
+  set_up<FIRST, FORM>(c, ws);
   if (gh && c.l.rows > 0) {
     c.a.grad_hidden = (char*)gh->data;
     c.a.gh_seq = gh->seq_stride * kSize<kDtype<FORM>>;
@@ -1242,13 +1241,12 @@ void gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc
     c.a.grad_head = (char*)gw->data;
     c.a.grad_row = gw->row_stride * kSize<kDtype<FORM>>;
   }
-  gather<FORM, kBackward>(c);
-  const char* whole = c.a.W.data;
+  gather<FIRST, FORM, kBackward>(c);
   const int d = c.a.d;
   for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
-    piece<FORM>(c, whole, (int)v0);
+    piece<FORM>(c, (int)v0);
     const int count = c.a.v1 - c.a.v0;
-    launch_product(excess_kernel<FORM>, c.a, most_tiles(c.l.rows, count), c.stream);
+    launch_product(excess_kernel<FIRST, FORM>, c.a, most_tiles(c.l.rows, count), c.stream);
     launch_product(grad_kernel<FORM>, c.a, (gh ? most_tiles(c.l.rows, d) * c.a.max_slices : 0) + (gw ? most_tiles(count, d) : 0), c.stream);
   }
   if (c.a.grad_hidden && c.a.max_slices > 1)
@@ -1305,12 +1303,12 @@ epic_status head_loss(bool backward, const epic_rows_desc* hidden, const int32_t
     c.g.grad_row = grad_hidden->row_stride * es;
   }
   char* ws = (char*)d_workspace;
-#define EPIC_HEAD(FORM) backward ? gradients<FORM>(c, ws, grad_hidden, grad_head) : losses<FORM>(c, ws, d_loss, d_lse)
-  switch (l.form) {
-    case kFormF32: losses<kFormF32>(c, ws, d_loss, d_lse); break;
-    case kFormSplit: EPIC_HEAD(kFormSplit); break;
-    case kFormF16: EPIC_HEAD(kFormF16); break;
-    default: EPIC_HEAD(kFormBf16);
+#define EPIC_HEAD(FIRST, FORM) backward ? gradients<FIRST, FORM>(c, ws, grad_hidden, grad_head) : losses<FIRST>(c, ws, d_loss, d_lse)
+  switch (l.first) {
+    case kFormF32: EPIC_HEAD(kFormF32, kFormSplit); break;
+    case kFormSplit: EPIC_HEAD(kFormSplit, kFormSplit); break;
+    case kFormF16: EPIC_HEAD(kFormF16, kFormF16); break;
+    default: EPIC_HEAD(kFormBf16, kFormBf16);
   }
 #undef EPIC_HEAD
   return hipGetLastError() == hipSuccess ? EPIC_OK : EPIC_ERR_HIP;
@@ -1398,9 +1396,9 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
   c.g.scale = (float*)(ws + l.scale);
   c.g.counts = (int2*)(ws + l.counts);
   switch (hidden->dtype) {
-    case EPIC_F32: gather<kFormF32, kQuantize>(c); break;
-    case EPIC_F16: gather<kFormF16, kQuantize>(c); break;
-    default: gather<kFormBf16, kQuantize>(c); break;
+    case EPIC_F32: gather<kFormF32, kFormF32, kQuantize>(c); break;
+    case EPIC_F16: gather<kFormF16, kFormF16, kQuantize>(c); break;
+    default: gather<kFormBf16, kFormBf16, kQuantize>(c); break;
   }
   HeadArgs& a = c.a;
   a.kept = c.g.kept;

@@ -1,7 +1,7 @@
 """A small denoiser trained on a teacher's top logits, then decoding under the
 grammar: the operators on logits rows together with the check.
 
-    python -m paper_2606_00722_amd.denoise [--preset 1] [--train 60] [--seed 42]
+    python -m paper_2606_00722_amd.denoise [--preset 1] [--train 60] [--seed 42] [--answers]
 
 The denoiser is one linear layer over fixed random features of every position,
 in the place of a network's last hidden states; the teacher's likeliest token is
@@ -10,6 +10,10 @@ which gives losses and the logits' gradient in one call.  A decoding step is
 sample, propose, validate, select and fallback (one commit where the selection
 is empty), all on the device; the host reads the number of candidates and
 whether masks are left.
+
+With --answers the denoiser learns the answers' tokens instead of a teacher's
+distribution, without logits (head_loss_forward and _backward), and decodes with
+its weights in 8 bits (quantize, logits_q8).
 """
 from __future__ import annotations
 
@@ -53,6 +57,41 @@ class Denoiser:
         return self.loss.sum() / masked.sum()
 
 
+class AnswerDenoiser:
+    """The same features as hidden states [B, n, d] in bfloat16 under a head
+    [V, d], kept in float32 and read in bfloat16; logits in bfloat16 from the
+    head in 8 bits.  No logits are kept for training."""
+
+    def __init__(self, B: int, n: int, V: int, device, gen):
+        import torch
+
+        d = max(64, B * n)
+        self.torch = torch
+        self.hidden = (torch.randn((B, n, d), generator=gen, device=device) / math.sqrt(d)).to(torch.bfloat16)
+        self.w = torch.zeros((V, d), device=device)
+        self.head = torch.zeros((V, d), dtype=torch.bfloat16, device=device)
+        self.grad = torch.empty_like(self.head)
+        self.out = torch.zeros((B, n, V), dtype=torch.bfloat16, device=device)
+        self.loss, self.lse = torch.empty((B, n), device=device), torch.empty((B, n), device=device)
+        self.q, self.scale = epic.alloc_q8(V, d, device)
+        self.ws = epic.alloc_head_loss_workspace(self.hidden, self.head)
+        self.ws8 = epic.alloc_logits_q8_workspace(self.hidden)
+
+    def train_step(self, seqs, target, lr: float):
+        """Mean loss over the masked positions (a device scalar)."""
+        epic.head_loss_forward(self.hidden, seqs, self.head, target, self.loss, self.lse, self.ws)
+        epic.head_loss_backward(self.hidden, seqs, self.head, target, self.lse, None, None, self.grad, self.ws)
+        self.w -= lr * self.grad.float()
+        self.head.copy_(self.w)
+        return self.loss.sum() / (seqs == W.MASK).sum()
+
+    def logits(self, seqs):
+        """Of the masked positions; the others' rows are not written."""
+        epic.quantize(self.head, self.q, self.scale)
+        epic.logits_q8(self.hidden, seqs, self.q, self.scale, self.out, self.ws8)
+        return self.out
+
+
 def teacher(hidden: np.ndarray, V: int, K: int, rng: np.random.Generator, device):
     """Top logits per position: the answer's token and K - 1 others, and their
     logsumexp with 5 % left to the tokens that are not listed."""
@@ -69,7 +108,7 @@ def teacher(hidden: np.ndarray, V: int, K: int, rng: np.random.Generator, device
     return tuple(torch.from_numpy(a).to(device) for a in (idx, logit, lse))
 
 
-def decode(ctx, model: Denoiser, seqs, gen, per_seq: int = 8, temperature: float = 0.8, top_k: int = 0, top_p: float = 0.95,
+def decode(ctx, model, seqs, gen, per_seq: int = 8, temperature: float = 0.8, top_k: int = 0, top_p: float = 0.95,
            max_steps: int = 500) -> int:
     """Fills the masks of seqs (int32 [B, n] on the GPU) in place; steps taken."""
     torch = model.torch
@@ -83,7 +122,8 @@ def decode(ctx, model: Denoiser, seqs, gen, per_seq: int = 8, temperature: float
     T, p = torch.full((B,), temperature, device=dev), torch.full((B,), top_p, device=dev)
     k, one = torch.full((B,), top_k, **i32), torch.ones(B, **i32)
     ws = ctx.alloc_workspace(dev)
-    logits = model.logits()  # of this denoiser they do not depend on what is committed
+    # of these denoisers logits do not depend on what is committed
+    logits = model.logits(seqs) if isinstance(model, AnswerDenoiser) else model.logits()
     for step in range(max_steps):
         if not bool((seqs == W.MASK).any()):
             return step
@@ -100,7 +140,8 @@ def decode(ctx, model: Denoiser, seqs, gen, per_seq: int = 8, temperature: float
     return max_steps
 
 
-def run(preset: int = 1, train: int = 60, seed: int = 42, lr: float = 4.0, log: Optional[Callable] = None) -> dict:
+def run(preset: int = 1, train: int = 60, seed: int = 42, lr: float = 4.0, log: Optional[Callable] = None,
+        answers: bool = False) -> dict:
     import torch
 
     dev = torch.device("cuda:0")
@@ -109,16 +150,19 @@ def run(preset: int = 1, train: int = 60, seed: int = 42, lr: float = 4.0, log: 
     inst = W.make_instance(preset, seed)
     ctx = epic.Context.from_problem(W.arrays(inst.lang, inst.vocab), inst.B, inst.n, 8 * inst.B)
     ctx.lexmemo_build()
-    model = Denoiser(inst.B, inst.n, inst.vocab.size, dev, gen)
+    model = (AnswerDenoiser if answers else Denoiser)(inst.B, inst.n, inst.vocab.size, dev, gen)
     seqs = torch.from_numpy(inst.seqs).to(dev)
-    top = teacher(inst.hidden, inst.vocab.size, 16, np.random.default_rng(seed), dev)
+    if answers:
+        goal = (torch.from_numpy(np.ascontiguousarray(inst.hidden, np.int32)).to(dev),)
+    else:
+        goal = teacher(inst.hidden, inst.vocab.size, 16, np.random.default_rng(seed), dev)
     losses: List[float] = []
     for i in range(train):
-        loss = model.train_step(seqs, *top, lr=lr)
+        loss = model.train_step(seqs, *goal, lr=lr)
         if i % 10 == 0 or i == train - 1:
             losses.append(float(loss))
             if log:
-                log(f"training step {i}: divergence {losses[-1]:.4f}")
+                log(f"training step {i}: {'loss' if answers else 'divergence'} {losses[-1]:.4f}")
     steps = decode(ctx, model, seqs, gen)
     filled = seqs.cpu().numpy()
     masked = inst.seqs == W.MASK
@@ -135,5 +179,6 @@ if __name__ == "__main__":
     a.add_argument("--preset", type=int, default=1, choices=sorted(W.PRESETS))
     a.add_argument("--train", type=int, default=60)
     a.add_argument("--seed", type=int, default=42)
+    a.add_argument("--answers", action="store_true", help="learn the answers' tokens, decode with the weights in 8 bits")
     args = a.parse_args()
-    run(args.preset, args.train, args.seed, log=lambda text: print(text, flush=True))
+    run(args.preset, args.train, args.seed, log=lambda text: print(text, flush=True), answers=args.answers)

@@ -200,10 +200,13 @@ def test_large(dtype, size, epic):
 
 
 @pytest.mark.parametrize("dtype", sorted(DT))
-def test_many_rows(dtype, epic):
-    """More rows that count than a tile has, by sums over all of them on the GPU in 64 bits."""
-    B, m, V, d = 8, 150, 1500, 192
-    c = Case(dtype, B, m, V, d, share=0.8, seed=3, weights="some")
+@pytest.mark.parametrize("size", [(8, 150, 1500, 192, 0.8), (4, 250, 20096, 256, 0.9), (6, 1000, 30016, 192, 0.3), (4, 64, 20032, 64, 0.5),
+                                  (2, 64, 9024, 448, 0.9), (9, 700, 26000, 72, 0.95), (3, 100, 4992, 1088, 1.0)], ids=str)
+def test_many_rows(dtype, size, epic):
+    """More rows that count than a tile has, every size of tile, several pieces of
+    the vocabulary and slices of them, by sums over all rows on the GPU in 64 bits."""
+    B, m, V, d, share = size
+    c = Case(dtype, B, m, V, d, share=share, seed=3, weights="some")
     loss, lse = forward(epic, c)
     gh, gw = backward(epic, c, lse)
     on = torch.from_numpy(c.on)
@@ -216,6 +219,7 @@ def test_many_rows(dtype, epic):
     G = p * c.weight[on].double().cuda()[:, None]
     u = U[c.dtype]
     P = torch.softmax(l, -1) * c.weight[on].double().cuda().abs()[:, None]
+    # (2^-25: half a step of float16's smallest numbers)
     bound = (G.abs() @ w.abs()) * (u + 8 * math.sqrt(V) * U32) + 2 * e * (P @ w.abs()) + (G @ w).abs() * u + 2.0 ** -25
     assert bool(((gh[on].cuda().double() - G @ w).abs() <= bound).all())
     bound = (G.abs().t() @ h.abs()) * (u + 8 * math.sqrt(len(y)) * U32) + 2 * e * (P.t() @ h.abs()) + (G.t() @ h).abs() * u
