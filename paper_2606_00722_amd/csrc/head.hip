@@ -47,9 +47,8 @@ struct GatherArgs {
   int64_t grad_seq, grad_row;
   Kept kept;
   char* out;         // packed rows
-  int64_t stride, plane;    // bytes
   char* out2;        // with the rows' powers of two, for the product over rows
-  int64_t stride2, plane2;
+  int64_t stride, plane;  // bytes
   int width;         // of packed rows, in numbers
   float* scale;      // 8 bits: the rows' scales
   const float* tops; // 32 bits: largest magnitudes of hidden states and head, in parts
@@ -237,9 +236,8 @@ EPIC_DEV void quantize_row(const char* row, int d, int8_t* out, int stride, floa
   }
 }
 
-// A row to packed numbers as FORM has them, multiplied with 2^e; with TWO also as
-// FORM2 has them, multiplied with 2^(e + e2).
-template <int FORM, int FORM2, bool TWO>
+// A row to packed numbers, multiplied with 2^e; with TWO also with 2^(e + e2).
+template <int FORM, bool TWO>
 EPIC_DEV void pack_row(const char* row, int d, int width, char* out, int64_t plane, int e, char* out2, int64_t plane2, int e2, int lane) {
   constexpr int N = 4;  // loads ahead
   for (int t0 = 0; t0 < width; t0 += 512 * N) {
@@ -257,8 +255,8 @@ EPIC_DEV void pack_row(const char* row, int d, int width, char* out, int64_t pla
       store8<FORM>(out, plane, t, x[j]);
       if constexpr (TWO) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[j][k] = __builtin_amdgcn_ldexpf(x[j][k], FORM == kFormSplit ? e2 : e + e2);
-        store8<FORM2>(out2, plane2, t, x[j]);
+        for (int k = 0; k < 8; ++k) x[j][k] = __builtin_amdgcn_ldexpf(x[j][k], e2);
+        store8<FORM>(out2, plane2, t, x[j]);
       }
     }
   }
@@ -290,7 +288,7 @@ __global__ void __launch_bounds__(256) count_kernel(GatherArgs a) {
 // 64 (the gradients' products sum over them).  Every workgroup counts the rows
 // before its own itself, so that one launch does it for up to 1024 rows; of more it
 // adds up count_kernel's numbers of 64 rows each.
-template <int FIRST, int FORM, int MODE>
+template <int FORM, int MODE>
 EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather / 64], int (&lds_own)[64], float (&lds_f)[kGather / 64]) {
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int total = a.batch * a.rows, first = group * a.per, last = min(total, first + a.per);
@@ -375,8 +373,8 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
           }
         }
         // a row that adds nothing has no numbers
-        pack_row<FIRST, FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.width, a.out + at * a.stride, a.plane, h_exp,
-                                        a.out2 + at * a.stride2, a.plane2, shift, lane);
+        pack_row<FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.width, a.out + at * a.stride, a.plane, h_exp,
+                                        a.out2 + at * a.stride, a.plane, shift, lane);
       }
     }
   }
@@ -385,11 +383,11 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
     if constexpr (kWeights)
       if (tid == 0) a.kept.count[1] = top_exp == -1000 ? 0 : top_exp;
     if constexpr (MODE == kBackward) {
-      const int end = (before + 63) / 64 * 64, vecs = (int)(a.stride2 / 16);
+      const int end = (before + 63) / 64 * 64, vecs = (int)(a.stride / 16);
       for (int i = tid; i < (end - before) * vecs; i += kGather) {
-        char* to = a.out2 + (int64_t)before * a.stride2 + (int64_t)i * 16;
+        char* to = a.out2 + (int64_t)before * a.stride + (int64_t)i * 16;
         *(uint4*)to = make_uint4(0, 0, 0, 0);
-        if constexpr (FORM == kFormSplit) *(uint4*)(to + a.plane2) = make_uint4(0, 0, 0, 0);
+        if constexpr (FORM == kFormSplit) *(uint4*)(to + a.plane) = make_uint4(0, 0, 0, 0);
       }
     }
   }
@@ -453,7 +451,7 @@ EPIC_DEV void pack_rows(const PackArgs& a, int group, int groups, float* lds) {
   int e_head = 0;
   if constexpr (FORM == kFormSplit) e_head = scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
   for (int i = group * 4 + wave; i < a.count; i += groups * 4)
-    pack_row<FORM, FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.width, a.out + i * a.stride, a.plane, e_head,
+    pack_row<FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.width, a.out + i * a.stride, a.plane, e_head,
                                 nullptr, 0, 0, lane);
 }
 template <int FORM>
@@ -464,13 +462,13 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a) {
 
 // The rows that count by the first `groups` workgroups, and by the others the
 // head's first piece where it has to be packed.
-template <int FIRST, int FORM, int MODE>
+template <int FORM, int MODE>
 __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a, PackArgs p, int groups) {
   __shared__ int lds_n[kGather / 64];
   __shared__ int lds_own[64];
   __shared__ float lds_f[kGather / 64];
   if ((int)blockIdx.x < groups)
-    gather_rows<FIRST, FORM, MODE>(a, (int)blockIdx.x, lds_n, lds_own, lds_f);
+    gather_rows<FORM, MODE>(a, (int)blockIdx.x, lds_n, lds_own, lds_f);
   else if constexpr (MODE != kQuantize)
     pack_rows<FORM>(p, (int)blockIdx.x - groups, (int)gridDim.x - groups, lds_f);
 }
@@ -487,8 +485,8 @@ __global__ void __launch_bounds__(256) quantize_kernel(const char* data, int64_t
 
 // ------------------------------------------------------------- products
 struct HeadArgs {
-  Operand H, W;      // rows that count [N, d], (a piece of) the head [v, d], for the logits
-  Operand H2, W2;    // and for the gradients
+  Operand H, W;      // rows that count [N, d], (a piece of) the head [v, d]
+  Operand H2;        // the rows as the head's gradient reads them
   Kept kept;
   int steps;         // of d
   int piece;         // tokens of a whole piece
@@ -676,18 +674,18 @@ __global__ void __launch_bounds__(256) loss_kernel(HeadArgs a, float* loss, floa
 // weights are in [1/2, 1): 2^-24 of p = 1 is a normal number.  Numbers of rows past
 // the last, of rows without a token (which have hidden states 0 and weight 0) and
 // of columns past the vocabulary are 0: the products that follow sum over them.
-template <int FIRST, int FORM, class T>
+template <int FORM, class T>
 EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* smem, int (&target)[2][256], float2 (&scale)[2][256]) {
   constexpr float kScale = kScaled<FORM> ? 16384.f : 1.f;
   const int m = ceil_div(count, T::BM), n = ceil_div(a.v1 - a.v0, T::BN);
   const float c = by * kLog2e;
   auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
-  every_tile<kPairs<FIRST>>(
+  every_tile<kPairs<FORM>>(
       t, smem, [&](int i) { return dealt(i, m * n); },
       [&](int id) {
         int tm, tn;
         place(id, tm, tn);
-        t.template start<kPairs<FIRST>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FIRST> == 3 ? kThreePairs : 0);
+        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FORM> == 3 ? kThreePairs : 0);
       },
       [&](int id, int k) {
         int tm, tn;
@@ -715,7 +713,7 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
         for (int i = 0; i < T::MT; ++i) {
           const int r = T::row(i, lane), at = tm * T::BM + r, y = target[k][r];
           const float2 x = scale[k][r];
-          char* row = const_cast<char*>(a.G.data) + at * a.G.stride + 2 * (int64_t)(tn * T::BN);
+          char* row = const_cast<char*>(a.G.data) + at * a.G.stride + kPacked<FORM> * (int64_t)(tn * T::BN);
           const bool some = __any((unsigned)(y - wn * (T::BN / T::WN)) < (unsigned)(T::BN / T::WN));
 #pragma unroll
           for (int j = 0; j < T::NT; j += T::F) {
@@ -739,21 +737,21 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
 #pragma unroll
             for (int h = 0; h < 4 * T::F; h += 8) {
               const float v[8] = {g[h], g[h + 1], g[h + 2], g[h + 3], g[h + 4], g[h + 5], g[h + 6], g[h + 7]};
-              store8<FORM>(row + 2 * c0, a.G.plane, h, v);
+              store8<FORM>(row + kPacked<FORM> * c0, a.G.plane, h, v);
             }
           }
         }
       });
 }
-template <int FIRST, int FORM>
+template <int FORM>
 __global__ void __launch_bounds__(kProductThreads) excess_kernel(HeadArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[kProductLds];
   __shared__ float lds_top[kProductThreads / 64];
   __shared__ int target[2][256];
   __shared__ float2 scale[2][256];  // lse in powers of two, and what 2^(l - lse) is multiplied with
   const int count = *a.kept.count;
-  const float by = unscale<FIRST>(a, lds_top);
-  with_size<Sizes<kKind<FIRST>, true, true>>(tile_size<kKind<FIRST>>(count, a.piece), [&](auto& t) { excess_tiles<FIRST, FORM>(a, t, count, by, smem, target, scale); });
+  const float by = unscale<FORM>(a, lds_top);
+  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { excess_tiles<FORM>(a, t, count, by, smem, target, scale); });
 }
 
 // ---- The two products with G, in one launch: the hidden states' gradient G W
@@ -808,7 +806,7 @@ EPIC_DEV void grad_hidden_tiles(const HeadArgs& a, T& t, const Split& s, int cou
         int tm, tn;
         const int slice = place(id, tm, tn);
         const int k0 = (int)((int64_t)all * slice / s.slices), k1 = (int)((int64_t)all * (slice + 1) / s.slices);
-        t.template start<P>(a.G, a.W2, tm * T::BM, tn * T::BN, m * T::BM, dp, k0, k1 - k0, P == 3 ? kThreePairs : 0);
+        t.template start<P>(a.G, a.W, tm * T::BM, tn * T::BN, m * T::BM, dp, k0, k1 - k0, P == 3 ? kThreePairs : 0);
       },
       [](int, int) {},
       [&](int id, int) {
@@ -945,6 +943,130 @@ __global__ void __launch_bounds__(256) scatter_kernel(HeadArgs a) {
   }
 }
 
+// ---- Both gradients of few float32 rows, on the vector units: G, hidden states
+// and head as they are.  Every wavefront works by itself on 256 columns.
+constexpr int kFewRows = 128, kFewCols = 256;
+
+// 16 rows' gradient over the `per` tokens of a slice.
+EPIC_DEV void few_hidden(const HeadArgs& a, int count, int id, int per, float* g, int lane) {
+  const int chunks = ceil_div(a.d, kFewCols), c = id % chunks * kFewCols + lane * 4;
+  // (the groups that there are one after another: every XCD has some)
+  const int slices = ceil_div(a.V, per), slice = id / chunks % slices, group = id / chunks / slices;
+  if (group * 16 >= count) return;
+  const int j0 = slice * per, j1 = min(a.V, j0 + per), c_in = min(c, a.d - 4);
+  const char* w_at = a.W.data + 4 * (int64_t)c_in;
+  constexpr int N = 8;  // loads ahead
+  f4 sum[16] = {}, w[N];
+  if (j0 < j1) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) w[u] = *(const f4*)(w_at + min(j0 + u, j1 - 1) * a.W.stride);
+  }
+  for (int t0 = j0; t0 < j1; t0 += 64) {
+    const int n = min(64, j1 - t0);
+    wait_lds();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {  // 16 rows of 64 tokens
+      const int r = k * 4 + (lane >> 4), t = (lane & 15) * 4;
+      const f4 x = *(const f4*)(a.G.data + (group * 16 + r) * a.G.stride + 4 * (int64_t)(t0 + t));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[(t + e) * 16 + r] = t + e < n ? x[e] : 0.f;
+    }
+    wait_lds();
+    for (int t = 0; t < n; t += N) {
+      f4 next[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) next[u] = *(const f4*)(w_at + min(t0 + t + N + u, j1 - 1) * a.W.stride);
+      __builtin_amdgcn_sched_barrier(0);  // the loads first
+      // (past the last token g is 0, and w the last token's)
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[r] += g[(t + u) * 16 + r] * w[u];
+#pragma unroll
+      for (int u = 0; u < N; ++u) w[u] = next[u];
+    }
+  }
+  if (c >= a.d) return;  // (d is a multiple of 64)
+#pragma unroll
+  for (int r = 0; r < 16; ++r) *(f4*)(a.dh + slice * a.dh_slice + (int64_t)(group * 16 + r) * a.width + c) = sum[r];
+}
+
+// TOKENS tokens' gradient over all rows.
+template <int TOKENS>
+EPIC_DEV void few_head(const HeadArgs& a, int count, int id, float* g, int lane) {
+  const int chunks = ceil_div(a.d, kFewCols), c = id % chunks * kFewCols + lane * 4, t0 = id / chunks * TOKENS;
+  if (t0 >= a.V) return;
+  const char* h_at = a.H.data + 4 * (int64_t)min(c, a.d - 4);
+  constexpr int N = 8;  // rows ahead
+  f4 sum[TOKENS] = {};
+  for (int r1 = 0; r1 < count; r1 += 32) {
+    wait_lds();
+#pragma unroll
+    for (int k = 0; k < TOKENS / 8; ++k) {  // 32 rows of so many tokens
+      const int r = k * (256 / TOKENS) + lane / (TOKENS / 4), t = lane % (TOKENS / 4) * 4;
+      const f4 x = *(const f4*)(a.G.data + min(r1 + r, count - 1) * a.G.stride + 4 * (int64_t)(t0 + t));
+      *(f4*)(g + r * TOKENS + t) = r1 + r < count ? x : f4{};
+    }
+    wait_lds();
+    for (int r0 = r1; r0 < min(count, r1 + 32); r0 += N) {  // (past the last row g is 0)
+      f4 h[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) h[u] = *(const f4*)(h_at + min(r0 + u, count - 1) * a.H.stride);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) sum[t] += g[(r0 - r1 + u) * TOKENS + t] * h[u];
+    }
+  }
+  if (c >= a.d) return;
+#pragma unroll
+  for (int t = 0; t < TOKENS; ++t)
+    if (t0 + t < a.V)
+      *(Loose16*)(a.grad_head + (t0 + t) * a.grad_row + 4 * (int64_t)c) =
+          Loose16{{__float_as_uint(sum[t][0]), __float_as_uint(sum[t][1]), __float_as_uint(sum[t][2]), __float_as_uint(sum[t][3])}};
+}
+
+// The first `hidden` wavefronts the one, the others the other.
+template <int TOKENS>
+__global__ void __launch_bounds__(256) few_kernel(HeadArgs a, int hidden, int per) {
+  __shared__ __attribute__((aligned(16))) float g[4][1024];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+  const int count = *a.kept.count, id = (int)blockIdx.x * 4 + wave;
+  if (id < hidden)
+    few_hidden(a, count, id, per, g[wave], lane);
+  else if (a.grad_head)
+    few_head<TOKENS>(a, count, id - hidden, g[wave], lane);
+}
+
+// The slices' sum to the hidden states' gradient: 256 columns of a row a
+// workgroup, a fourth of the slices each wavefront.
+__global__ void __launch_bounds__(256) few_sum_kernel(HeadArgs a, int slices) {
+  __shared__ f4 part[4][64];
+  const int chunks = ceil_div(a.d, 256), at = (int)blockIdx.x / chunks, lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const int c = (int)blockIdx.x % chunks * 256 + lane * 4;
+  if (at >= *a.kept.count) return;
+  f4 sum = {};
+  if (c < a.d) {
+    const float* p = a.dh + (int64_t)at * a.width + c;
+    for (int s0 = wave; s0 < slices; s0 += 32) {
+      f4 x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = *(const f4*)(p + min(s0 + 4 * u, slices - 1) * a.dh_slice);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (s0 + 4 * u < slices) sum += x[u];
+    }
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave != 0 || c >= a.d) return;
+  sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+  const int r = a.kept.src[at], b = r / a.rows;
+  const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
+  store4<EPIC_F32>(a.grad_hidden + b * a.gh_seq + (r - b * a.rows) * a.gh_row, c, a.d, x);
+}
+
 // Logits of a head in 8 bits: sums of whole numbers, exact in 32 bits, times the
 // row's and the token's scale.
 template <int DT, class T>
@@ -1030,9 +1152,8 @@ inline int64_t most_tiles(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + 1
 struct Layout {
   int64_t rows, padded;  // rows of the window, and up to a multiple of 256
   int64_t width;         // of packed rows, in numbers
-  int first, form;       // of the logits' product, of the gradients' (the same but for few float32 rows)
-  bool direct;           // the head is read where it is, for the logits,
-  bool packed;           // or (and) written out
+  int form;              // of the products
+  bool direct;           // the head is read where it is
   int64_t piece;         // tokens of a piece
   int max_slices;        // of a piece's tokens, in the hidden states' gradient
   int64_t parts;
@@ -1047,13 +1168,15 @@ bool head_direct(const epic_rows_desc* head) {
          ((uintptr_t)head->data & 15) == 0;
 }
 
-// Logits of few float32 rows multiply numbers as they are: reading the head for
-// its largest magnitude and writing it out in two parts takes longer than the
-// slower products (losses, 32768 tokens of width 2048: 64 rows 91 us, in two parts
-// 274; 512 rows 500 and 416).  Both passes do so: exp(l - lse) is to have the
-// errors of one l.
+// Few float32 rows are multiplied as they are: finding the head's largest magnitude
+// and writing it out in two parts takes longer than slower products.  Losses and
+// gradients in us, so and in two parts: 64 rows, 32768 tokens of width 2048 95 + 421
+// and 285 + 510 (128 rows: 158 + 803 and 244 + 492), 128 rows with 64 that count, 512
+// tokens of width 128 45 and 56 (100 rows, 4096 tokens of width 1024: 48 + 90 and 43
+// + 73).
 bool as_it_is(const epic_rows_desc* hidden, const epic_rows_desc* head) {
-  return hidden->dtype == EPIC_F32 && (int64_t)hidden->batch * hidden->rows <= 128 && head_direct(head);
+  const int64_t rows = (int64_t)hidden->batch * hidden->rows, size = (int64_t)head->rows * head->vocab;
+  return hidden->dtype == EPIC_F32 && head_direct(head) && (rows <= 64 || (rows <= kFewRows && size <= 1 << 19));
 }
 
 Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool backward) {
@@ -1062,16 +1185,13 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.rows = (int64_t)hidden->batch * hidden->rows;
   l.padded = up(l.rows, 256);
   l.width = up(hidden->vocab, 64);
-  l.form = hidden->dtype == EPIC_F32 ? kFormSplit : hidden->dtype == EPIC_F16 ? kFormF16 : kFormBf16;
-  l.first = as_it_is(hidden, head) ? kFormF32 : l.form;
-  const bool split = l.form == kFormSplit;
-  l.direct = split ? l.first == kFormF32 : head_direct(head);
-  l.packed = !l.direct || (split && backward);
-  const int planes = split ? 2 : 1;
+  l.form = as_it_is(hidden, head) ? kFormF32 : hidden->dtype == EPIC_F32 ? kFormSplit : hidden->dtype == EPIC_F16 ? kFormF16 : kFormBf16;
+  l.direct = l.form != kFormSplit && head_direct(head);
+  const int planes = l.form == kFormSplit ? 2 : 1, es = l.form == kFormF32 ? 4 : 2;
   l.piece = up(V, 256);
-  if (backward || l.packed) {
+  if (backward || !l.direct) {
     // 128 MiB of G, 256 of the head, but not less than a launch takes to fill the CUs
-    const int64_t wide = std::max<int64_t>(l.packed ? (l.width + 1) / 2 : 0, backward ? l.padded : 0);
+    const int64_t wide = std::max<int64_t>(l.direct ? 0 : (l.width + 1) / 2, backward ? l.padded : 0);
     const int64_t most = std::max<int64_t>(4096, (1 << 26) / std::max<int64_t>(1, wide * planes) / 256 * 256);
     const int64_t pieces = (V + most - 1) / most;
     l.piece = up((V + pieces - 1) / pieces, 256);
@@ -1085,6 +1205,8 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   };
   // slices of the hidden states' gradient: 128 MiB of them, or one
   l.max_slices = l.piece < 2048 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, (1 << 25) / std::max<int64_t>(1, l.padded * l.width)));
+  if (l.form == kFormF32)  // wavefronts for every CU, of at least 16 tokens
+    l.max_slices = (int)std::max<int64_t>(1, std::min<int64_t>((V + 15) / 16, 2048 / ((l.rows + 15) / 16 * ((l.width + kFewCols - 1) / kFewCols) + 1)));
   l.counts = take((l.padded + 63) / 64 * 8);
   l.count = take(8);
   l.src = take(4 * l.padded);
@@ -1094,15 +1216,15 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.exp = take(4 * l.padded);
   l.tops = take(8 * kTopParts);
   l.at_target = take(4 * l.padded);
-  const int64_t whole = 2 * planes * l.width;  // bytes of a packed row in all its planes
-  l.H = take(l.padded * (l.first == kFormF32 ? 4 * l.width : whole));
-  if (l.packed) l.W = take(l.piece * whole);
+  const int64_t whole = es * planes * l.width;  // bytes of a packed row in all its planes
+  l.H = take(l.padded * whole);
+  if (!l.direct) l.W = take(l.piece * whole);
   if (!backward) {
     l.part = take(8 * l.padded * l.parts);
   } else {
-    l.H2 = l.form == kFormBf16 ? l.H : take(l.padded * whole);
-    l.G = take(2 * planes * l.padded * l.piece);
-    l.dh = take(4 * l.max_slices * l.padded * l.width);
+    l.H2 = l.form == kFormF16 || l.form == kFormSplit ? take(l.padded * whole) : l.H;
+    l.G = take(es * planes * l.padded * l.piece);
+    l.dh = take(4 * (l.form == kFormF32 ? l.max_slices * kFewRows : l.max_slices * l.padded) * l.width);
   }
   l.bytes = at;
   return l;
@@ -1134,12 +1256,12 @@ struct Call {
 template <int FORM>
 PackArgs pack_args(const Call& c, int v0) {
   return {(const char*)c.head->data, c.head->row_stride * kSize<kDtype<FORM>>, c.head->rows, c.head->vocab, v0,
-          (int)up(std::min<int64_t>(c.head->rows - v0, c.l.piece), 64), const_cast<char*>(c.a.W2.data), c.a.W2.stride, c.a.W2.plane,
+          (int)up(std::min<int64_t>(c.head->rows - v0, c.l.piece), 64), const_cast<char*>(c.a.W.data), c.a.W.stride, c.a.W.plane,
           (int)c.l.width, c.a.tops, {c.a.top_parts[0], c.a.top_parts[1]}};
 }
 inline int pack_groups(const PackArgs& p) { return std::min(2048, (p.count + 3) / 4); }
 
-template <int FIRST, int FORM, int MODE>
+template <int FORM, int MODE>
 void gather(Call& c) {
   c.g.per = (int)std::max<int64_t>(4, up((c.l.rows + 4095) / 4096, 4));
   const int groups = (int)std::max<int64_t>(1, (c.l.rows + c.g.per - 1) / c.g.per);
@@ -1150,16 +1272,16 @@ void gather(Call& c) {
   else
     hipLaunchKernelGGL(count_kernel, dim3((int)((c.l.rows + 255) / 256)), dim3(256), 0, c.stream, c.g);
   if constexpr (MODE != kQuantize) {
-    if (FORM == kFormSplit && (FIRST == kFormSplit || MODE == kBackward)) {
+    if (FORM == kFormSplit) {
       TopArgs t{c.g, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
       hipLaunchKernelGGL(top_kernel, dim3(c.g.top_parts[0] + c.g.top_parts[1]), dim3(256), 0, c.stream, t);
     }
-    if (c.l.packed) {
+    if (!c.l.direct) {
       p = pack_args<FORM>(c, 0);
       more = pack_groups(p);
     }
   }
-  hipLaunchKernelGGL((gather_kernel<FIRST, FORM, MODE>), dim3(groups + more), dim3(kGather), 0, c.stream, c.g, p, groups);
+  hipLaunchKernelGGL((gather_kernel<FORM, MODE>), dim3(groups + more), dim3(kGather), 0, c.stream, c.g, p, groups);
 }
 
 // The head's piece from token v0 on.
@@ -1169,10 +1291,8 @@ void piece(Call& c, int v0) {
   c.a.v1 = (int)std::min<int64_t>(c.a.V, v0 + c.l.piece);
   c.a.last = c.a.v1 == c.a.V;
   c.a.add = v0 > 0;
-  const char* raw = (const char*)c.head->data + v0 * c.head->row_stride * elem_size(c.head->dtype);
-  if (c.l.direct) c.a.W.data = raw;
-  if (!c.l.packed) {
-    c.a.W2.data = raw;
+  if (c.l.direct) {
+    c.a.W.data = (const char*)c.head->data + v0 * c.a.W.stride;
   } else if (v0 > 0) {
     const PackArgs p = pack_args<FORM>(c, v0);
     hipLaunchKernelGGL(pack_kernel<FORM>, dim3(pack_groups(p)), dim3(256), 0, c.stream, p);
@@ -1180,29 +1300,29 @@ void piece(Call& c, int v0) {
 }
 
 // What both passes set up: operands, rows that count, the head's pieces.
-template <int FIRST, int FORM>
+template <int FORM>
 void set_up(Call& c, char* ws) {
   const Layout& l = c.l;
   Kept kept{(int32_t*)(ws + l.count), (int32_t*)(ws + l.src), (int32_t*)(ws + l.target), (float*)(ws + l.lse), (float*)(ws + l.mul),
             (int32_t*)(ws + l.exp)};
-  const int64_t es = kPacked<FIRST>, stride = es * l.width, plane = l.padded * stride, stride2 = 2 * l.width, plane2 = l.padded * stride2;
+  constexpr int64_t es = kPacked<FORM>;
+  const int64_t stride = es * l.width, plane = l.padded * stride;
   c.g.kept = c.a.kept = kept;
   c.g.counts = (int2*)(ws + l.counts);
   c.g.out = ws + l.H;
   c.g.stride = stride;
   c.g.plane = plane;
   c.g.out2 = ws + l.H2;
-  c.g.stride2 = stride2;
-  c.g.plane2 = plane2;
   c.g.tops = c.a.tops = (float*)(ws + l.tops);
   c.g.top_parts[0] = c.a.top_parts[0] = (int)std::min<int64_t>(kTopParts, (l.rows + 3) / 4);
   c.g.top_parts[1] = c.a.top_parts[1] = std::min(kTopParts, (c.head->rows + 3) / 4);
   c.a.H = {ws + l.H, stride, plane};
-  c.a.H2 = {ws + l.H2, stride2, plane2};
-  const Operand raw{(const char*)c.head->data, c.head->row_stride * es, 0}, written{ws + l.W, stride2, l.piece * stride2};
-  c.a.W = l.direct ? raw : written;
-  c.a.W2 = l.packed ? written : raw;
-  c.a.G = {ws + l.G, 2 * l.piece, 2 * l.padded * l.piece};
+  c.a.H2 = {ws + l.H2, stride, plane};
+  if (l.direct)
+    c.a.W = {(const char*)c.head->data, c.head->row_stride * es, 0};
+  else
+    c.a.W = {ws + l.W, stride, l.piece * stride};
+  c.a.G = {ws + l.G, es * l.piece, es * l.padded * l.piece};
   c.a.steps = (int)(stride / 128);
   c.a.V = c.head->rows;
   c.a.d = c.head->vocab;
@@ -1217,11 +1337,10 @@ void set_up(Call& c, char* ws) {
   c.a.rows = c.hidden->rows;
 }
 
-// FORM: of the logits' product.
 template <int FORM>
 void losses(Call& c, char* ws, float* loss, float* lse) {
-  set_up<FORM, FORM>(c, ws);
-  gather<FORM, FORM, kForward>(c);
+  set_up<FORM>(c, ws);
+  gather<FORM, kForward>(c);
   for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
     piece<FORM>(c, (int)v0);
     launch_product(lse_kernel<FORM>, c.a, most_tiles(c.l.rows, c.a.v1 - c.a.v0), c.stream);
@@ -1229,9 +1348,9 @@ void losses(Call& c, char* ws, float* loss, float* lse) {
   hipLaunchKernelGGL(loss_kernel<FORM>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a, loss, lse);
 }
 
-template <int FIRST, int FORM>
+template <int FORM>
 void gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc* gw) {
-  set_up<FIRST, FORM>(c, ws);
+  set_up<FORM>(c, ws);
   if (gh && c.l.rows > 0) {
     c.a.grad_hidden = (char*)gh->data;
     c.a.gh_seq = gh->seq_stride * kSize<kDtype<FORM>>;
@@ -1241,16 +1360,31 @@ void gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc
     c.a.grad_head = (char*)gw->data;
     c.a.grad_row = gw->row_stride * kSize<kDtype<FORM>>;
   }
-  gather<FIRST, FORM, kBackward>(c);
+  gather<FORM, kBackward>(c);
   const int d = c.a.d;
-  for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
-    piece<FORM>(c, (int)v0);
-    const int count = c.a.v1 - c.a.v0;
-    launch_product(excess_kernel<FIRST, FORM>, c.a, most_tiles(c.l.rows, count), c.stream);
-    launch_product(grad_kernel<FORM>, c.a, (gh ? most_tiles(c.l.rows, d) * c.a.max_slices : 0) + (gw ? most_tiles(count, d) : 0), c.stream);
+  if constexpr (FORM == kFormF32) {  // of so few rows G is one piece
+    piece<FORM>(c, 0);
+    launch_product(excess_kernel<FORM>, c.a, most_tiles(c.l.rows, c.a.V), c.stream);
+    const int chunks = (d + kFewCols - 1) / kFewCols, per = (int)up((c.a.V + c.l.max_slices - 1) / c.l.max_slices, 16),
+              slices = (c.a.V + per - 1) / per;
+    c.a.dh_slice = kFewRows * c.l.width;
+    const int waves = c.a.grad_hidden ? chunks * (kFewRows / 16) * slices : 0;
+    // 32 tokens a wavefront take the least from LDS and the rows; of few tokens less, for more wavefronts
+    const bool wide = (int64_t)chunks * c.a.V >= 32 * 1024;
+    const int tokens = wide ? 32 : 8, more = gw ? chunks * ((c.a.V + tokens - 1) / tokens) : 0;
+    hipLaunchKernelGGL(wide ? few_kernel<32> : few_kernel<8>, dim3((waves + more + 3) / 4), dim3(256), 0, c.stream, c.a, waves, per);
+    if (waves)
+      hipLaunchKernelGGL(few_sum_kernel, dim3((int)c.l.rows * ((d + 255) / 256)), dim3(256), 0, c.stream, c.a, slices);
+  } else {
+    for (int64_t v0 = 0; v0 < c.a.V; v0 += c.l.piece) {
+      piece<FORM>(c, (int)v0);
+      const int count = c.a.v1 - c.a.v0;
+      launch_product(excess_kernel<FORM>, c.a, most_tiles(c.l.rows, count), c.stream);
+      launch_product(grad_kernel<FORM>, c.a, (gh ? most_tiles(c.l.rows, d) * c.a.max_slices : 0) + (gw ? most_tiles(count, d) : 0), c.stream);
+    }
+    if (c.a.grad_hidden && c.a.max_slices > 1)
+      hipLaunchKernelGGL(scatter_kernel<FORM>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a);
   }
-  if (c.a.grad_hidden && c.a.max_slices > 1)
-    hipLaunchKernelGGL(scatter_kernel<FORM>, dim3((int)((c.l.rows + 3) / 4)), dim3(256), 0, c.stream, c.a);
 }
 
 epic_status head_loss(bool backward, const epic_rows_desc* hidden, const int32_t* d_seqs, int32_t n, const int32_t* d_start,
@@ -1303,12 +1437,12 @@ epic_status head_loss(bool backward, const epic_rows_desc* hidden, const int32_t
     c.g.grad_row = grad_hidden->row_stride * es;
   }
   char* ws = (char*)d_workspace;
-#define EPIC_HEAD(FIRST, FORM) backward ? gradients<FIRST, FORM>(c, ws, grad_hidden, grad_head) : losses<FIRST>(c, ws, d_loss, d_lse)
-  switch (l.first) {
-    case kFormF32: EPIC_HEAD(kFormF32, kFormSplit); break;
-    case kFormSplit: EPIC_HEAD(kFormSplit, kFormSplit); break;
-    case kFormF16: EPIC_HEAD(kFormF16, kFormF16); break;
-    default: EPIC_HEAD(kFormBf16, kFormBf16);
+#define EPIC_HEAD(FORM) backward ? gradients<FORM>(c, ws, grad_hidden, grad_head) : losses<FORM>(c, ws, d_loss, d_lse)
+  switch (l.form) {
+    case kFormF32: EPIC_HEAD(kFormF32); break;
+    case kFormSplit: EPIC_HEAD(kFormSplit); break;
+    case kFormF16: EPIC_HEAD(kFormF16); break;
+    default: EPIC_HEAD(kFormBf16);
   }
 #undef EPIC_HEAD
   return hipGetLastError() == hipSuccess ? EPIC_OK : EPIC_ERR_HIP;
@@ -1396,9 +1530,9 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
   c.g.scale = (float*)(ws + l.scale);
   c.g.counts = (int2*)(ws + l.counts);
   switch (hidden->dtype) {
-    case EPIC_F32: gather<kFormF32, kFormF32, kQuantize>(c); break;
-    case EPIC_F16: gather<kFormF16, kFormF16, kQuantize>(c); break;
-    default: gather<kFormBf16, kFormBf16, kQuantize>(c); break;
+    case EPIC_F32: gather<kFormF32, kQuantize>(c); break;
+    case EPIC_F16: gather<kFormF16, kQuantize>(c); break;
+    default: gather<kFormBf16, kQuantize>(c); break;
   }
   HeadArgs& a = c.a;
   a.kept = c.g.kept;
