@@ -50,6 +50,7 @@ struct GatherArgs {
   char* out2;        // with the rows' powers of two, for the product over rows
   int64_t stride, plane;  // bytes
   int width;         // of packed rows, in numbers
+  int shift;         // of their last 64
   float* scale;      // 8 bits: the rows' scales
   const float* tops; // 32 bits: largest magnitudes of hidden states and head, in parts
   int top_parts[2];
@@ -236,14 +237,20 @@ EPIC_DEV void quantize_row(const char* row, int d, int8_t* out, int stride, floa
   }
 }
 
-// A row to packed numbers, multiplied with 2^e; with TWO also with 2^(e + e2).
+// A row to packed numbers, multiplied with 2^e; with TWO also with 2^(e + e2).  The
+// last 64 are zeros and numbers `shift` further on where the row has so few that
+// the head, read where it is, has to be read up to its end (a multiple of 8).
 template <int FORM, bool TWO>
-EPIC_DEV void pack_row(const char* row, int d, int width, char* out, int64_t plane, int e, char* out2, int64_t plane2, int e2, int lane) {
+EPIC_DEV void pack_row(const char* row, int d, int width, int shift, char* out, int64_t plane, int e, char* out2, int64_t plane2, int e2, int lane) {
   constexpr int N = 4;  // loads ahead
   for (int t0 = 0; t0 < width; t0 += 512 * N) {
     float x[N][8];
 #pragma unroll
-    for (int j = 0; j < N; ++j) load8<kDtype<FORM>>(row, t0 + j * 512 + lane * 8, d, x[j]);
+    for (int j = 0; j < N; ++j) {
+      int t = t0 + j * 512 + lane * 8;
+      if (t >= width - 64) t = t - shift < width - 64 ? d : t - shift;
+      load8<kDtype<FORM>>(row, t, d, x[j]);
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int t = t0 + j * 512 + lane * 8;
@@ -373,7 +380,7 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
           }
         }
         // a row that adds nothing has no numbers
-        pack_row<FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.width, a.out + at * a.stride, a.plane, h_exp,
+        pack_row<FORM, kWeights>(row, MODE == kBackward && y < 0 ? 0 : a.d, a.width, a.shift, a.out + at * a.stride, a.plane, h_exp,
                                         a.out2 + at * a.stride, a.plane, shift, lane);
       }
     }
@@ -451,7 +458,7 @@ EPIC_DEV void pack_rows(const PackArgs& a, int group, int groups, float* lds) {
   int e_head = 0;
   if constexpr (FORM == kFormSplit) e_head = scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
   for (int i = group * 4 + wave; i < a.count; i += groups * 4)
-    pack_row<FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.width, a.out + i * a.stride, a.plane, e_head,
+    pack_row<FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.width, 0, a.out + i * a.stride, a.plane, e_head,
                                 nullptr, 0, 0, lane);
 }
 template <int FORM>
@@ -491,6 +498,8 @@ struct HeadArgs {
   int steps;         // of d
   int piece;         // tokens of a whole piece
   int width;         // d up to a multiple of 64
+  int shift;         // of the last 64 of hidden states: the head is read where it is, up to its rows' end
+  bool direct;
   int v0, v1;        // tokens of the piece
   int V, d;
   // losses
@@ -574,7 +583,8 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
       [&](int id) {
         int tm, tn;
         place(id, tm, tn);
-        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FORM> == 3 ? kThreePairs : 0);
+        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FORM> == 3 ? kThreePairs : 0,
+                                         1 << 30, 2 * a.shift);
       },
       [&](int id, int k) {
         int tm, tn;
@@ -685,7 +695,8 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
       [&](int id) {
         int tm, tn;
         place(id, tm, tn);
-        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FORM> == 3 ? kThreePairs : 0);
+        t.template start<kPairs<FORM>>(a.H, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.v1 - a.v0, 0, a.steps, kPairs<FORM> == 3 ? kThreePairs : 0,
+                                         1 << 30, 2 * a.shift);
       },
       [&](int id, int k) {
         int tm, tn;
@@ -806,7 +817,8 @@ EPIC_DEV void grad_hidden_tiles(const HeadArgs& a, T& t, const Split& s, int cou
         int tm, tn;
         const int slice = place(id, tm, tn);
         const int k0 = (int)((int64_t)all * slice / s.slices), k1 = (int)((int64_t)all * (slice + 1) / s.slices);
-        t.template start<P>(a.G, a.W, tm * T::BM, tn * T::BN, m * T::BM, dp, k0, k1 - k0, P == 3 ? kThreePairs : 0);
+        t.template start<P>(a.G, a.W, tm * T::BM, tn * T::BN, m * T::BM, a.direct ? a.d : dp, k0, k1 - k0, P == 3 ? kThreePairs : 0,
+                            a.direct ? a.v1 - a.v0 : 1 << 30);
       },
       [](int, int) {},
       [&](int id, int) {
@@ -880,7 +892,11 @@ EPIC_DEV void grad_head_tiles(const HeadArgs& a, T& t, const Split& s, int count
           char* row = a.grad_head + v * a.grad_row;
 #pragma unroll
           for (int j = 0; j < T::NT; ++j) {
-            const int c = tn * T::BN + T::col(j, lane);
+            int c = tn * T::BN + T::col(j, lane);
+            if (c >= a.width - 64 && a.shift) {
+              if (c - a.shift < a.width - 64) continue;  // zeros
+              c -= a.shift;
+            }
             float g[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) g[k] = !kScaled<FORM> ? t.acc[i][j][k] : __builtin_amdgcn_ldexpf(t.acc[i][j][k], e);
@@ -1160,11 +1176,10 @@ struct Layout {
   int64_t counts, count, src, target, lse, mul, exp, tops, at_target, part, H, H2, W, G, dh, bytes;
 };
 
-// The products read a head in its place when its rows are whole steps and tiles
-// of vectors.
+// The products read a head in its place when its rows are vectors of 16 bytes.
 bool head_direct(const epic_rows_desc* head) {
   const int per = 16 / elem_size(head->dtype);
-  return head->vocab % 64 == 0 && head->rows % 64 == 0 && head->row_stride % per == 0 && head->row_stride < (1 << 20) &&
+  return head->vocab % 8 == 0 && head->vocab >= 64 && head->row_stride % per == 0 && head->row_stride < (1 << 20) &&
          ((uintptr_t)head->data & 15) == 0;
 }
 
@@ -1176,7 +1191,7 @@ bool head_direct(const epic_rows_desc* head) {
 // + 73).
 bool as_it_is(const epic_rows_desc* hidden, const epic_rows_desc* head) {
   const int64_t rows = (int64_t)hidden->batch * hidden->rows, size = (int64_t)head->rows * head->vocab;
-  return hidden->dtype == EPIC_F32 && head_direct(head) && (rows <= 64 || (rows <= kFewRows && size <= 1 << 19));
+  return hidden->dtype == EPIC_F32 && head_direct(head) && head->vocab % 64 == 0 && (rows <= 64 || (rows <= kFewRows && size <= 1 << 19));
 }
 
 Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool backward) {
@@ -1334,6 +1349,8 @@ void set_up(Call& c, char* ws) {
   c.a.max_slices = l.max_slices;
   c.a.piece = (int)l.piece;
   c.a.width = c.g.width = (int)l.width;
+  c.a.shift = c.g.shift = l.direct ? (int)(l.width - c.head->vocab) : 0;
+  c.a.direct = l.direct;
   c.a.parts = l.parts;
   c.a.rows = c.hidden->rows;
 }

@@ -172,7 +172,8 @@ def _p_sizes(c):
 SIZES = [  # B, m, V, d, pad, window
     (1, 1, 1, 1, 0, False), (1, 1, 2, 3, 1, False), (1, 3, 63, 64, 0, False), (2, 5, 64, 65, 3, True),
     (1, 17, 257, 63, 0, True), (3, 11, 300, 128, 8, False), (2, 64, 256, 64, 0, False), (2, 65, 1025, 127, 1, True),
-    (5, 33, 640, 320, 0, True)]
+    (5, 33, 640, 320, 0, True), (2, 40, 257, 72, 0, False), (3, 33, 1003, 136, 8, True), (2, 70, 514, 1000, 0, False), (1, 9, 67, 64, 0, False),
+    (2, 33, 130, 120, 8, False)]
 
 
 @pytest.mark.parametrize("dtype", sorted(DT))
@@ -200,7 +201,7 @@ def test_large(dtype, size, epic):
 
 
 MANY = [(8, 150, 1500, 192, 0.8), (4, 250, 20096, 256, 0.9), (6, 1000, 30016, 192, 0.3), (4, 64, 20032, 64, 0.5), (2, 64, 9024, 448, 0.9),
-        (9, 700, 26000, 72, 0.95), (3, 100, 4992, 1088, 1.0)]
+        (9, 700, 26000, 72, 0.95), (3, 100, 4992, 1088, 1.0), (4, 700, 20011, 264, 0.9), (2, 300, 9999, 1032, 0.9), (2, 90, 30001, 200, 0.8)]
 # (the last: a head that is written out in pieces for the losses too)
 MANY = [(dt, size) for size in MANY for dt in sorted(DT)] + [("bfloat16", (1, 90, 70001, 1999, 0.5)), ("float32", (1, 70, 40000, 1990, 0.9))]
 
