@@ -499,12 +499,19 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
  * their way through the sums; an infinite logit gives NaN.
  *
  * The gradients go by pieces of the vocabulary: a piece's logits are computed
- * again from the forward pass's lse, G is kept for one piece, and two products
- * read it.  Sums are float32.  16-bit inputs are multiplied as they are, and G
- * is rounded to their type; of float32 inputs and their G the products take 22
- * bits and a sign, relative to numbers of at least 2^-17 of the tensor's largest
- * (smaller ones: 2^-40 of it).  float16 G is scaled so that exp(l - lse) from
- * 2^-24 on is a normal number, whatever the weight.
+ * again and set against the forward pass's lse, G is kept for one piece (256 MiB
+ * of it, or 4096 tokens), and two products read it.  Sums are float32.  16-bit
+ * inputs are multiplied as they are, and G is rounded to their type; float16 G
+ * is scaled so that exp(l - lse) from 2^-24 on is a normal number, whatever the
+ * weight.  Up to 64 float32 rows (128 of small heads) are multiplied in float32;
+ * of more the products take 22 bits and a sign, relative to numbers of at least
+ * 2^-17 of the tensor's largest (smaller ones: 2^-40 of it), G as well.  A logit
+ * whose product with log2(e) is past float32 counts as infinite.
+ *
+ * A head whose rows are 16-byte vectors (its address and row_stride in bytes
+ * multiples of 16, its width a multiple of 8 and at least 64; float32 beyond 64
+ * rows not) is read where it is, another is written out in the workspace first,
+ * which takes as long as two readings of it.
  *
  * d_loss and d_lse float32 [batch*rows].  d_weight float32 [batch*rows]: the
  * upstream gradient of each row's loss (NULL: 1).  grad_hidden (shape and type
