@@ -503,7 +503,8 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
  * of it, or 4096 tokens), and two products read it.  Sums are float32.  16-bit
  * inputs are multiplied as they are, and G is rounded to their type; float16 G
  * is scaled so that exp(l - lse) from 2^-24 on is a normal number, whatever the
- * weight.  Up to 64 float32 rows (128 of small heads) are multiplied in float32;
+ * weight; in grad_head its rows' hidden states are multiplied with their weights'
+ * powers of two over the largest one's, where products below 2^-14 lose bits.  Up to 64 float32 rows (128 of small heads) are multiplied in float32;
  * of more the products take 22 bits and a sign, relative to numbers of at least
  * 2^-17 of the tensor's largest (smaller ones: 2^-40 of it), G as well.  A logit
  * whose product with log2(e) is past float32 counts as infinite.

@@ -277,6 +277,13 @@ EPIC_DEV void zero_grad(char* row, int d, int lane) {
 
 enum GatherMode { kForward, kBackward, kQuantize };
 
+// The power of two of a row's weight, -1000 where there is none: of 0, of what is no
+// number, and in rows that add nothing.
+EPIC_DEV int weight_exp(const GatherArgs& a, int r) {
+  const float w = a.weight ? a.weight[r] : 1.f;
+  return w != 0.f && fabsf(w) < kInf && !(a.target && a.target[r] >= a.V) ? __builtin_amdgcn_frexp_expf(w) : -1000;
+}
+
 // Of every 64 rows of the window how many count, and the largest power of two of
 // their weights: one wavefront each.
 __global__ void __launch_bounds__(256) count_kernel(GatherArgs a) {
@@ -284,8 +291,7 @@ __global__ void __launch_bounds__(256) count_kernel(GatherArgs a) {
   const int total = a.batch * a.rows, r = group * 64 + lane;
   if (group * 64 >= total) return;
   const bool on = r < total && kept_row(a, r);
-  const float w = on && a.weight ? a.weight[r] : 1.f;
-  const int e = on && w != 0.f && fabsf(w) < kInf ? __builtin_amdgcn_frexp_expf(w) : -1000;
+  const int e = on ? weight_exp(a, r) : -1000;
   const int n = (int)__popcll(__ballot(on));
   const float top = wave_max((float)e);
   if (lane == 0) a.counts[group] = make_int2(n, (int)top);
@@ -317,10 +323,7 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
     for (int r = tid; r < (kWeights ? total : first); r += kGather)
       if (kept_row(a, r)) {
         before += r < first;
-        if constexpr (kWeights) {
-          const float w = a.weight ? a.weight[r] : 1.f;
-          if (w != 0.f && fabsf(w) < kInf) top_exp = max(top_exp, __builtin_amdgcn_frexp_expf(w));
-        }
+        if constexpr (kWeights) top_exp = max(top_exp, weight_exp(a, r));
       }
   }
   before = (int)wave_sum((float)(before & 0xFFF)) + ((int)wave_sum((float)(before >> 12)) << 12);
@@ -370,7 +373,7 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
         if constexpr (MODE == kBackward) {
           float w = a.weight ? a.weight[r] : 1.f;
           int e = 0;
-          if (kWeights && w != 0.f && fabsf(w) < kInf) {
+          if (kWeights && weight_exp(a, r) > -1000) {
             e = __builtin_amdgcn_frexp_expf(w);
             shift = e - top_exp;
             w = __builtin_amdgcn_frexp_mantf(w);

@@ -273,6 +273,22 @@ def test_tokens_outside_the_vocabulary(dtype, epic):
     assert torch.allclose(gw.float(), gw2.float(), rtol=4 * U[dtype], atol=float(want[5].max()) * 2 * U[dtype])
 
 
+@pytest.mark.parametrize("rows", [90, 1100])
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_weight_of_a_row_that_adds_nothing(dtype, rows, epic):
+    """However large it is, the others' gradients are those without the row."""
+    c = Case(dtype, 1, rows, 70, 40, share=1.0, seed=6)
+    c.target[0, rows - 5] = c.V
+    c.full_h[0, rows - 5] = 1.0
+    c.weight[0, rows - 5] = 1e30
+    c.on = head_ref.counted(1, rows, c.seqs, None, c.target)
+    _, lse = forward(epic, c)
+    gh, gw = backward(epic, c, lse)
+    c.weight[0, rows - 5] = 0
+    gh2, gw2 = backward(epic, c, lse)
+    assert torch.equal(gh, gh2) and torch.equal(gw, gw2) and bool(gw.any())
+
+
 @pytest.mark.parametrize("dtype", sorted(DT))
 def test_not_a_number_stays_in_its_row(dtype, epic):
     c = Case(dtype, 2, 8, 100, 64, share=1.0)
