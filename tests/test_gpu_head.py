@@ -202,8 +202,11 @@ def test_large(dtype, size, epic):
 
 MANY = [(8, 150, 1500, 192, 0.8), (4, 250, 20096, 256, 0.9), (6, 1000, 30016, 192, 0.3), (4, 64, 20032, 64, 0.5), (2, 64, 9024, 448, 0.9),
         (9, 700, 26000, 72, 0.95), (3, 100, 4992, 1088, 1.0), (4, 700, 20011, 264, 0.9), (2, 300, 9999, 1032, 0.9), (2, 90, 30001, 200, 0.8)]
-# (the last: a head that is written out in pieces for the losses too)
-MANY = [(dt, size) for size in MANY for dt in sorted(DT)] + [("bfloat16", (1, 90, 70001, 1999, 0.5)), ("float32", (1, 70, 40000, 1990, 0.9))]
+MANY = [(dt, size) for size in MANY for dt in sorted(DT)]
+# a head that is written out in pieces for the losses too; the largest vocabulary and width; a great many rows
+MANY += [("bfloat16", (1, 90, 70001, 1999, 0.5)), ("float32", (1, 70, 40000, 1990, 0.9)), ("bfloat16", (1, 20, 262144, 64, 1.0)),
+         ("float32", (1, 20, 262144, 64, 1.0)), ("float16", (1, 5, 100, 65536, 1.0)), ("float32", (1, 5, 100, 65536, 1.0)),
+         ("bfloat16", (3, 100000, 40, 16, 0.5)), ("float32", (2, 50000, 70, 24, 0.5))]
 
 
 @pytest.mark.parametrize("dtype,size", MANY, ids=str)
