@@ -535,7 +535,8 @@ struct HeadArgs {
 // small result into more pieces and keep more loads of the head on their way.
 // Which, the kernel decides, by how many rows count.  Losses of 32768 tokens of width
 // 2048 in bfloat16, large, mid and few, in us: 16 rows 57, 34, 34; 128 rows 54, 35, 39;
-// 256 rows 55, 51, 65; 512 rows 66, 89, 115.
+// 256 rows 55, 51, 65; 512 rows 66, 89, 115.  Of the few rows that are multiplied in
+// float32 the smallest tiles are best (16 rows 91 us, in mid tiles 152, large 484).
 template <int KIND, bool A_ALONG, bool B_ALONG>
 struct Sizes {
   typedef Tile<KIND, 256, 256, 2, 4, 2, A_ALONG, B_ALONG> Large;
@@ -550,22 +551,27 @@ EPIC_DEV int ceil_div(int a, int b) { return (a + b - 1) / b; }
 EPIC_DEV int tile_cost(int size) { return size == 0 ? 20 : size == 1 ? 9 : 6; }
 template <int KIND>
 EPIC_DEV int tile_size(int m, int n, int copies = 1) {
+  if (KIND == kF32) return 2;
   const auto rounds = [&](int rows, int cols) { return ((int64_t)ceil_div(m, rows) * ceil_div(n, cols) * copies + kCus - 1) / kCus; };
-  const int64_t c0 = rounds(256, 256) * (KIND == kF32 ? 32 : 20), c1 = rounds(128, 128) * 9, c2 = rounds(64, 128) * (KIND == kF32 ? 5 : 6);
+  const int64_t c0 = rounds(256, 256) * tile_cost(0), c1 = rounds(128, 128) * tile_cost(1), c2 = rounds(64, 128) * tile_cost(2);
   return c2 < c1 && c2 < c0 ? 2 : c1 < c0 ? 1 : 0;
 }
 template <class S, class F>
 EPIC_DEV void with_size(int size, F&& f) {
-  if (size == 0) {
-    typename S::Large t;
-    f(t);
-  } else if (size == 1) {
-    typename S::Mid t;
-    f(t);
-  } else {
-    typename S::Few t;
-    f(t);
+  if constexpr (S::Few::KIND != kF32) {
+    if (size == 0) {
+      typename S::Large t;
+      f(t);
+      return;
+    }
+    if (size == 1) {
+      typename S::Mid t;
+      f(t);
+      return;
+    }
   }
+  typename S::Few t;
+  f(t);
 }
 
 // What sums of products are multiplied with to be logits.
@@ -1407,7 +1413,8 @@ void gradients(Call& c, char* ws, const epic_rows_desc* gh, const epic_rows_desc
               slices = (c.a.V + per - 1) / per;
     c.a.dh_slice = kFewRows * c.l.width;
     const int waves = c.a.grad_hidden ? chunks * (kFewRows / 16) * slices : 0;
-    // 32 tokens a wavefront take the least from LDS and the rows; of few tokens less, for more wavefronts
+    // 32 tokens a wavefront take the least from LDS and the rows; of small heads 8, for
+    // more wavefronts (64 rows, 512 tokens, width 128: 9 us, with 32 31)
     const bool wide = (int64_t)chunks * c.a.V >= 32 * 1024;
     const int tokens = wide ? 32 : 8, more = gw ? chunks * ((c.a.V + tokens - 1) / tokens) : 0;
     hipLaunchKernelGGL(wide ? few_kernel<32> : few_kernel<8>, dim3((waves + more + 3) / 4), dim3(256), 0, c.stream, c.a, waves, per);

@@ -486,9 +486,15 @@ def distill_backward(logits, seqs, top_idx, top_logit, stats, weight, grad, star
 
 
 def _matrix(name, t, device=None) -> _Rows:
-    if t.dim() != 2:
-        raise ValueError(f"{name}: a [V, d] tensor, got {tuple(t.shape)}")
-    return _rows(name, t.unsqueeze(0), device)
+    if t.dim() != 2 or t.dtype not in _dtypes():
+        raise ValueError(f"{name}: a [V, d] tensor of float32, float16 or bfloat16, got {tuple(t.shape)} {t.dtype}")
+    V, d = t.shape
+    sv, sd = t.stride()
+    if sd != 1 and d > 1:
+        raise ValueError(f"{name}: a row's numbers have to be adjacent, got strides {t.stride()}")
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise ValueError(f"{name}: on {t.device}, needs a GPU tensor" + ("" if device is None else f" on cuda:{device}"))
+    return _Rows(t.data_ptr(), _DTYPES[t.dtype], 1, V, d, V * sv, sv)
 
 
 def _scratch(workspace, device):
