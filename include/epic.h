@@ -504,15 +504,19 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
  * inputs are multiplied as they are, and G is rounded to their type; float16 G
  * is scaled so that exp(l - lse) from 2^-24 on is a normal number, whatever the
  * weight; in grad_head its rows' hidden states are multiplied with their weights'
- * powers of two over the largest one's, where products below 2^-14 lose bits.  Up to 64 float32 rows (128 of small heads) are multiplied in float32;
- * of more the products take 22 bits and a sign, relative to numbers of at least
- * 2^-17 of the tensor's largest (smaller ones: 2^-40 of it), G as well.  A logit
- * whose product with log2(e) is past float32 counts as infinite.
+ * powers of two over the largest one's, where products below 2^-14 lose bits.
+ * Up to 64 float32 rows (128 where the head has at most 2^19 numbers) are
+ * multiplied in float32, if the head is read where it is and its width is a
+ * multiple of 64.  In all other float32 calls the products take 22 bits and a
+ * sign, relative to numbers of at least 2^-17 of the tensor's largest (smaller
+ * ones: 2^-40 of it), G as well.  A logit whose product with log2(e) is past
+ * float32 counts as infinite.
  *
- * A head whose rows are 16-byte vectors (its address and row_stride in bytes
- * multiples of 16, its width a multiple of 8 and at least 64; float32 beyond 64
- * rows not) is read where it is, another is written out in the workspace first,
- * which takes as long as two readings of it.
+ * A head is read where it is if its rows are 16-byte vectors (its address and
+ * row_stride in bytes multiples of 16, row_stride below 2^20 numbers), its width is
+ * a multiple of 8 and at least 64, and the products are not those of 22 bits;
+ * another is written out in the workspace first, which takes as long as two
+ * readings of it.
  *
  * d_loss and d_lse float32 [batch*rows].  d_weight float32 [batch*rows]: the
  * upstream gradient of each row's loss (NULL: 1).  grad_hidden (shape and type
