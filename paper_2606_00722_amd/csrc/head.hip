@@ -222,7 +222,7 @@ EPIC_DEV void quantize_row(const char* row, int d, int8_t* out, int stride, floa
   const float inv = odd || top < 1e-30f ? 0.f : 127.f / top;
   if (lane == 0) *scale = odd ? __builtin_nanf("") : inv == 0.f ? 0.f : top / 127.f;
   for (int t0 = 0; t0 < stride; t0 += 512 * N) {
-    if (d > 512 * N) load(t0);
+    if (t0 > 0 || d > 512 * N) load(t0);  // (zeros behind the row)
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int t = t0 + j * 512 + lane * 8;
