@@ -406,9 +406,11 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
 }
 
 // Largest finite magnitudes of the hidden states' rows that count (the first
-// workgroups) and of the head, one number a workgroup.
+// workgroups; for gradients without rows that add nothing) and of the head, one
+// number a workgroup.
 struct TopArgs {
   GatherArgs g;
+  bool gradients;
   const char* head;
   int64_t head_row;
   float* tops;
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
     if (head) {
       row = a.head + r * a.head_row;
     } else {
-      if (!kept_row(a.g, r)) continue;
+      if (!kept_row(a.g, r) || (a.gradients && a.g.target[r] >= a.g.V)) continue;
       const int b = r / a.g.rows;
       row = a.g.data + b * a.g.seq_stride + (r - b * a.g.rows) * a.g.row_stride;
     }
@@ -1315,7 +1317,7 @@ void gather(Call& c) {
     hipLaunchKernelGGL(count_kernel, dim3((int)((c.l.rows + 255) / 256)), dim3(256), 0, c.stream, c.g);
   if constexpr (MODE != kQuantize) {
     if (FORM == kFormSplit) {
-      TopArgs t{c.g, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
+      TopArgs t{c.g, MODE == kBackward, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
       hipLaunchKernelGGL(top_kernel, dim3(c.g.top_parts[0] + c.g.top_parts[1]), dim3(256), 0, c.stream, t);
     }
     if (!c.l.direct) {

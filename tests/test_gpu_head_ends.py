@@ -3,7 +3,7 @@ may be."""
 import pytest
 
 from tests import head_ref
-from tests.test_gpu_head import DT, epic  # noqa: F401 (epic: a fixture)
+from tests.test_gpu_head import DT, Case, backward, epic, forward  # noqa: F401 (epic: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +27,21 @@ def test_quantize_to_any_stride(dtype, d, stride, epic):  # noqa: F811
     want_q, want_s = head_ref.quantize(x)
     assert torch.equal(q.cpu()[:, :d].float(), want_q) and torch.equal(s.cpu(), want_s)
     assert not bool(q[:, d:].any())
+
+
+# ------------------------------------------------ rows that add nothing
+
+
+@pytest.mark.parametrize("rows", [90, 1100])
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_hidden_states_of_a_row_that_adds_nothing(dtype, rows, epic):  # noqa: F811
+    """However large they are, the others' gradients are those without the row."""
+    c = Case(dtype, 1, rows, 70, 40, share=1.0, seed=6)
+    c.target[0, rows - 5] = c.V
+    c.on = head_ref.counted(1, rows, c.seqs, None, c.target)
+    c.full_h[0, rows - 5] = 1.0
+    _, lse = forward(epic, c)
+    want = backward(epic, c, lse)
+    c.full_h[0, rows - 5] = 60000.0 if dtype == "float16" else 1e30
+    got = backward(epic, c, lse)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool(got[1].any())
