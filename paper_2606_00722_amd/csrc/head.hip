@@ -584,10 +584,13 @@ EPIC_DEV float unscale(const HeadArgs& a, float* lds) {
   return __builtin_amdgcn_ldexpf(1.f, -e);
 }
 
+constexpr float kFar = 16777216.f;  // of a logit in powers of two: it is rounded to whole numbers
+
 // Losses: a tile's columns to a maximum and a sum for every row, over the wavefronts of a
 // row of tiles by LDS, and the logit of the row's token.  exp2 takes one product
 // and sum: with c = log2(e) (and what unscales sums) t c is rounded to T, and the
-// sum of 2^(l c - T) is too large by the factor 2^(t c - T), which is taken out.
+// sum of 2^(l c - T) is too large by the factor 2^(t c - T), which is taken out.  Past
+// 2^31 that factor can leave float32: from kFar on a term is 2^((l - t) c).
 // 2867 rows of 32768 tokens, width 2048, in bfloat16: 333 us, 1.16 PFLOP/s (the ends
 // of 32-step tiles take a tenth); 16 rows of 131072 tokens, width 4096: 180 us, bound
 // by reading the head at 6.0 TB/s.
@@ -641,14 +644,22 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
           top = fmaxf(top, __shfl_xor(top, 16));  // the four lanes of a row
           top = fmaxf(top, __shfl_xor(top, 32));
           const float base = top > -kInf ? top : 0.f, tc = base * c;
+          const bool far = __any(fabsf(tc) >= kFar);
           float sum = 0.f;
+          if (far) {
 #pragma unroll
-          for (int j = 0; j < T::NT; ++j)
+            for (int j = 0; j < T::NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][e], c, -tc));
+              for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((t.acc[i][j][e] - base) * c);
+          } else {
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][e], c, -tc));
+          }
           sum += __shfl_xor(sum, 16);
           sum += __shfl_xor(sum, 32);
-          if (lane < 16) part[wn * T::BM + r] = make_float2(top * by, sum * __builtin_amdgcn_exp2f(-__builtin_fmaf(base, c, -tc)));
+          if (lane < 16) part[wn * T::BM + r] = make_float2(top * by, far ? sum : sum * __builtin_amdgcn_exp2f(-__builtin_fmaf(base, c, -tc)));
         }
         lds_barrier();
         for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
@@ -746,6 +757,7 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
           const int r = T::row(i, lane), at = tm * T::BM + r, y = target[k][r];
           const float2 x = scale[k][r];
           char* row = const_cast<char*>(a.G.data) + at * a.G.stride + kPacked<FORM> * (int64_t)(tn * T::BN);
+          const bool far = __any(fabsf(x.x) >= kFar);
           const bool some = __any((unsigned)(y - wn * (T::BN / T::WN)) < (unsigned)(T::BN / T::WN));
 #pragma unroll
           for (int j = 0; j < T::NT; j += T::F) {
@@ -753,6 +765,12 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
 #pragma unroll
             for (int f = 0; f < 4 * T::F; ++f)
               g[f] = x.y * __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j + f / 4][f & 3], c, -x.x));
+            if (far) {  // the factors' product could leave float32
+              const float lse = at < count ? a.kept.lse[at] : 0.f, w = at < count ? a.kept.mul[at] * kScale : 0.f;
+#pragma unroll
+              for (int f = 0; f < 4 * T::F; ++f)
+                g[f] = w * __builtin_amdgcn_exp2f((t.acc[i][j + f / 4][f & 3] * by - lse) * kLog2e);
+            }
             const int c0 = T::col(j, lane);
             if (some && (unsigned)(y - c0) < (unsigned)(4 * T::F)) {  // 1 - p without what p = 1 rounds away
               float l = 0.f;

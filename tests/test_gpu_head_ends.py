@@ -1,9 +1,16 @@
 """The operators between hidden states and logits at the ends of what their inputs
-may be."""
+may be: strides above the least, rows that add nothing, logits past 2^31.
+
+Tolerances as in test_gpu_head (u32 = 2^-24), by row: a row's logits are off by
+(8 sqrt(d) u32 + 2^-22) of its largest sum A of terms' magnitudes, its lse by that, 2e-5 and,
+where it is large, the roundings of a float32 number of its size (lse's sum, the loss's
+difference: 4 u32 |lse| for both)."""
+import math
+
 import pytest
 
 from tests import head_ref
-from tests.test_gpu_head import DT, Case, backward, epic, forward  # noqa: F401 (epic: a fixture)
+from tests.test_gpu_head import DT, U32, Case, backward, epic, forward  # noqa: F401 (epic: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +52,56 @@ def test_hidden_states_of_a_row_that_adds_nothing(dtype, rows, epic):  # noqa: F
     c.full_h[0, rows - 5] = 60000.0 if dtype == "float16" else 1e30
     got = backward(epic, c, lse)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool(got[1].any())
+
+
+# ------------------------------------------------------- large logits
+
+
+def by_row(c, lse):
+    """Bounds of every row's logits, and of lse and loss [B, m]."""
+    h, w = c.h.double(), c.w.double()
+    A = torch.zeros((c.B, c.m), dtype=torch.float64)
+    on = torch.from_numpy(c.on)
+    A[on] = (h[on].abs() @ w.abs().t()).amax(-1)
+    off = (8 * math.sqrt(c.d) * U32 + (2.0 ** -22 if c.dtype == "float32" else 0.0)) * A
+    return off, off + 2e-5 + 4 * U32 * lse.abs()
+
+
+@pytest.mark.parametrize("dtype,m", [("bfloat16", 6), ("float16", 6), ("float32", 6), ("float32", 70)])
+def test_logits_past_two_to_the_31(dtype, m, epic):  # noqa: F811
+    """One token of 2^35 and more in every row: it has probability 1, the others 0."""
+    V, d = 300, 128
+    c = Case(dtype, 2, m, V, d, share=1.0, seed=14)
+    g = torch.Generator().manual_seed(15)
+    c.full_h[..., :d] = (2.0 ** 14 * (1 + torch.rand((2, m, d), generator=g))).to(DT[dtype])
+    c.full_w[:, :d] = (torch.randn((V, d), generator=g)).to(DT[dtype])
+    c.full_w[5] = (2.0 ** 14 * (1 + torch.rand(d, generator=g))).to(DT[dtype])
+    c.target = torch.randint(6, V, (2, m), generator=g).to(torch.int32)
+    c.target[:, ::2] = 5
+    c.on = head_ref.counted(2, m, c.seqs, None, c.target)
+    loss, lse = forward(epic, c)
+    want = head_ref.loss(c.h, c.w, c.target, c.on, c.weight)
+    off, _ = by_row(c, want[1])
+    e = off + 4 * U32 * want[1]
+    assert bool((want[1] > 2.0 ** 34).all())
+    assert bool(((lse.cpu() - want[1]).abs() <= e).all()) and bool(((loss.cpu() - want[0]).abs() <= 2 * e).all())
+    assert not bool(loss[:, ::2].any())
+    gh, gw = backward(epic, c, lse)
+    # G is the row's weight at token 5 and minus it at the row's own, each rounded to the type, as the result
+    w = c.w.double()
+    diff, size = w[5] - w[c.target.long()], w[5].abs() + w[c.target.long()].abs()
+    u = torch.finfo(DT[dtype]).eps / 2 if dtype != "float32" else 2.0 ** -22
+    weight = c.weight.double()[..., None]
+    lim = torch.finfo(DT[dtype]).max
+    got, want_h = gh.double(), (diff * weight)
+    assert bool(((got - want_h).abs() <= 3 * u * size * weight.abs())[want_h.abs() < 0.9 * lim].all())
+    assert not bool(gh[:, ::2].any())
+    G = torch.zeros((2 * m, V), dtype=torch.float64)
+    G[:, 5] += c.weight.double().reshape(-1)
+    G[torch.arange(2 * m), c.target.reshape(-1).long()] -= c.weight.double().reshape(-1)
+    h = c.h.double().reshape(2 * m, d)
+    want_w, size_w = G.t() @ h, G.abs().t() @ h.abs()
+    left = 2 * m * float((c.weight.abs().max() * c.h.abs().max())) * (2.0 ** -38 if dtype == "float32" else 0.0) \
+        + (2.0 ** -25 + 4 * m * float(c.weight.abs().max()) * 2.0 ** -25 if dtype == "float16" else 0.0)
+    bad = ~((gw.double() - want_w).abs() <= 3 * u * size_w + 8 * math.sqrt(2 * m) * U32 * size_w + left) & (want_w.abs() < 0.9 * lim)
+    assert not bool(bad.any())
