@@ -508,9 +508,11 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
  * Up to 64 float32 rows (128 where the head has at most 2^19 numbers) are
  * multiplied in float32, if the head is read where it is and its width is a
  * multiple of 64.  In all other float32 calls the products take 22 bits and a
- * sign, relative to numbers of at least 2^-17 of the tensor's largest (smaller
- * ones: 2^-40 of it), G as well.  A logit whose product with log2(e) is past
- * float32 counts as infinite.
+ * sign of numbers from 2^-17 of the largest one on, and of smaller ones what is
+ * above 2^-40 of it.  The largest one is a row's own in hidden states, the whole
+ * head's in the head, and the row's weight for G; in grad_head rows' hidden states
+ * come with their weights, and the largest one is that of all rows that add
+ * something.  A logit whose product with log2(e) is past float32 counts as infinite.
  *
  * A head is read where it is if its rows are 16-byte vectors (its address and
  * row_stride in bytes multiples of 16, row_stride below 2^20 numbers), its width is

@@ -31,6 +31,7 @@ struct Kept {
   float* lse;       // backward
   float* mul;       // backward: what the row's part of the gradient is multiplied with before it is rounded
   int32_t* exp;     // backward: and the power of two after the products
+  int32_t* scale;   // 32 bits in two parts: the power of two of the packed row
 };
 
 struct GatherArgs {
@@ -52,8 +53,7 @@ struct GatherArgs {
   int width;         // of packed rows, in numbers
   int shift;         // of their last 64
   float* scale;      // 8 bits: the rows' scales
-  const float* tops; // 32 bits: largest magnitudes of hidden states and head, in parts
-  int top_parts[2];
+  int32_t* row_exp;  // 32 bits in two parts: powers of two of the rows' largest magnitudes, or NULL
   int per;           // rows of a workgroup
   int2* counts;      // of every 64 rows, or NULL
   int V;
@@ -94,8 +94,8 @@ EPIC_DEV uint32_t pack_f16(float a, float b) {
 EPIC_DEV uint32_t pack_bf16(float a, float b) {
   return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
 }
-// A 32-bit number as the sum of two 16-bit ones.  With the tensor's largest
-// magnitude scaled to [2^14, 2^15), numbers down to 2^-17 of it keep 22 bits and
+// A 32-bit number as the sum of two 16-bit ones.  With the largest magnitude (of a
+// row of hidden states, of the head) scaled to [2^14, 2^15), numbers down to 2^-17 of it keep 22 bits and
 // a sign (the second one's half step: 2^-24 of the number), smaller ones an
 // error of 2^-40 of the largest.
 EPIC_DEV void split_f16(float x, _Float16& a, _Float16& b) {
@@ -168,8 +168,11 @@ EPIC_DEV void put8(char* row, int t, int d, const float (&x)[8]) {
   }
 }
 
-// The power of two that scales a largest magnitude to [2^14, 2^15).
-EPIC_DEV int scale_exp(float top) { return top > 0.f ? 15 - (__builtin_amdgcn_frexp_expf(top)) : 0; }
+// e with 2^(e - 1) <= |x| < 2^e, kNoExp of 0; and the power of two that scales such a
+// number to [2^14, 2^15).
+constexpr int kNoExp = -1000;
+EPIC_DEV int exp_of(float x) { return x != 0.f ? __builtin_amdgcn_frexp_expf(x) : kNoExp; }
+EPIC_DEV int scale_exp(int e) { return e == kNoExp ? 0 : 15 - e; }
 
 EPIC_DEV float block_max(float v, float* lds) {
   v = wave_max(v);
@@ -277,21 +280,29 @@ EPIC_DEV void zero_grad(char* row, int d, int lane) {
 
 enum GatherMode { kForward, kBackward, kQuantize };
 
-// The power of two of a row's weight, -1000 where there is none: of 0, of what is no
+// The power of two of a row's weight, kNoExp where there is none: of 0, of what is no
 // number, and in rows that add nothing.
 EPIC_DEV int weight_exp(const GatherArgs& a, int r) {
   const float w = a.weight ? a.weight[r] : 1.f;
-  return w != 0.f && fabsf(w) < kInf && !(a.target && a.target[r] >= a.V) ? __builtin_amdgcn_frexp_expf(w) : -1000;
+  return fabsf(w) < kInf && !(a.target && a.target[r] >= a.V) ? exp_of(w) : kNoExp;
+}
+// That of what the row brings to a sum over rows: of its weight, and where rows are
+// scaled each by itself of its largest magnitude too.
+EPIC_DEV int part_exp(const GatherArgs& a, int r) {
+  const int e = weight_exp(a, r);
+  if (!a.row_exp || e == kNoExp) return e;
+  const int m = a.row_exp[r];
+  return m == kNoExp ? kNoExp : e + m;
 }
 
 // Of every 64 rows of the window how many count, and the largest power of two of
-// their weights: one wavefront each.
+// what they bring: one wavefront each.
 __global__ void __launch_bounds__(256) count_kernel(GatherArgs a) {
   const int group = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   const int total = a.batch * a.rows, r = group * 64 + lane;
   if (group * 64 >= total) return;
   const bool on = r < total && kept_row(a, r);
-  const int e = on ? weight_exp(a, r) : -1000;
+  const int e = on ? part_exp(a, r) : kNoExp;
   const int n = (int)__popcll(__ballot(on));
   const float top = wave_max((float)e);
   if (lane == 0) a.counts[group] = make_int2(n, (int)top);
@@ -310,7 +321,7 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
   constexpr int DT = kDtype<FORM>;
   constexpr bool kWeights = MODE == kBackward && kScaled<FORM>;
   int before = 0, top_exp = INT32_MIN;
-  // (the powers of two of the rows' weights go by the largest one)
+  // (the powers of two of what the rows bring go by the largest one)
   if (a.counts) {
     const int mine = first / 64, groups = kWeights ? (total + 63) / 64 : mine;
     for (int g = tid; g < groups; g += kGather) {
@@ -323,11 +334,11 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
     for (int r = tid; r < (kWeights ? total : first); r += kGather)
       if (kept_row(a, r)) {
         before += r < first;
-        if constexpr (kWeights) top_exp = max(top_exp, weight_exp(a, r));
+        if constexpr (kWeights) top_exp = max(top_exp, part_exp(a, r));
       }
   }
   before = (int)wave_sum((float)(before & 0xFFF)) + ((int)wave_sum((float)(before >> 12)) << 12);
-  if constexpr (kWeights) top_exp = (int)wave_max((float)max(top_exp, -1000));
+  if constexpr (kWeights) top_exp = (int)wave_max((float)max(top_exp, kNoExp));
   if (lane == 0) {
     lds_n[wave] = before;
     lds_f[wave] = (float)top_exp;
@@ -337,8 +348,6 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
   for (int w = 0; w < kGather / 64; ++w) before += lds_n[w];
   if constexpr (kWeights)
     for (int w = 0; w < kGather / 64; ++w) top_exp = max(top_exp, (int)lds_f[w]);
-  int h_exp = 0;
-  if constexpr (FORM == kFormSplit && MODE != kQuantize) h_exp = scale_exp(top_of(a.tops, a.top_parts[0], lds_f));
   for (int base = first; base < last; base += 64) {
     const int n = min(64, last - base);
     __syncthreads();
@@ -368,14 +377,18 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
       } else {
         int y = a.target[r];
         if (y >= a.V) y = -2;
-        if (lane == 0) a.kept.target[at] = y;
-        int shift = 0;
+        int h_exp = 0, shift = 0;
+        if constexpr (FORM == kFormSplit) h_exp = scale_exp(a.row_exp[r]);
+        if (lane == 0) {
+          a.kept.target[at] = y;
+          if constexpr (FORM == kFormSplit) a.kept.scale[at] = h_exp;
+        }
         if constexpr (MODE == kBackward) {
           float w = a.weight ? a.weight[r] : 1.f;
           int e = 0;
-          if (kWeights && weight_exp(a, r) > -1000) {
-            e = __builtin_amdgcn_frexp_expf(w);
-            shift = e - top_exp;
+          if (kWeights && weight_exp(a, r) != kNoExp) {
+            e = exp_of(w);
+            shift = part_exp(a, r) == kNoExp ? 0 : part_exp(a, r) - top_exp;
             w = __builtin_amdgcn_frexp_mantf(w);
           }
           if (lane == 0) {
@@ -393,7 +406,7 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
   if (last == total) {
     if (tid == 0) *a.kept.count = before;
     if constexpr (kWeights)
-      if (tid == 0) a.kept.count[1] = top_exp == -1000 ? 0 : top_exp;
+      if (tid == 0) a.kept.count[1] = top_exp == kNoExp ? 0 : top_exp;
     if constexpr (MODE == kBackward) {
       const int end = (before + 63) / 64 * 64, vecs = (int)(a.stride / 16);
       for (int i = tid; i < (end - before) * vecs; i += kGather) {
@@ -405,21 +418,20 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
   }
 }
 
-// Largest finite magnitudes of the hidden states' rows that count (the first
-// workgroups; for gradients without rows that add nothing) and of the head, one
-// number a workgroup.
+// The powers of two of the largest finite magnitudes: of every row of hidden states
+// that counts (the first workgroups), and of the head, a number for each of the others.
 struct TopArgs {
   GatherArgs g;
-  bool gradients;
   const char* head;
   int64_t head_row;
   float* tops;
+  int row_groups;
 };
 __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
   __shared__ float lds[4];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
-  const bool head = (int)blockIdx.x >= a.g.top_parts[0];
-  const int part = head ? (int)blockIdx.x - a.g.top_parts[0] : (int)blockIdx.x, parts = a.g.top_parts[head];
+  const bool head = (int)blockIdx.x >= a.row_groups;
+  const int part = head ? (int)blockIdx.x - a.row_groups : (int)blockIdx.x, parts = head ? (int)gridDim.x - a.row_groups : a.row_groups;
   const int total = head ? a.g.V : a.g.batch * a.g.rows;
   constexpr int N = 4;  // loads ahead
   float top = 0.f;
@@ -428,9 +440,10 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
     if (head) {
       row = a.head + r * a.head_row;
     } else {
-      if (!kept_row(a.g, r) || (a.gradients && a.g.target[r] >= a.g.V)) continue;
+      if (!kept_row(a.g, r)) continue;
       const int b = r / a.g.rows;
       row = a.g.data + b * a.g.seq_stride + (r - b * a.g.rows) * a.g.row_stride;
+      top = 0.f;
     }
     for (int t0 = 0; t0 < a.g.d; t0 += 512 * N) {
       float x[N][8];
@@ -442,9 +455,14 @@ __global__ void __launch_bounds__(256) top_kernel(TopArgs a) {
         for (int e = 0; e < 8; ++e)
           if (fabsf(x[j][e]) < kInf) top = fmaxf(top, fabsf(x[j][e]));
     }
+    if (!head) {
+      top = wave_max(top);
+      if (lane == 0) a.g.row_exp[r] = exp_of(top);
+    }
   }
+  if (!head) return;
   top = block_max(top, lds);
-  if (threadIdx.x == 0) a.tops[blockIdx.x] = top;
+  if (threadIdx.x == 0) a.tops[part] = top;
 }
 
 // Rows v0 .. of the head as the products read them, one wavefront a row: widths
@@ -456,14 +474,14 @@ struct PackArgs {
   char* out;
   int64_t stride, plane;
   int width;
-  const float* tops;
-  int top_parts[2];
+  const float* tops;  // 32 bits: the head's largest magnitudes, in parts
+  int top_parts;
 };
 template <int FORM>
 EPIC_DEV void pack_rows(const PackArgs& a, int group, int groups, float* lds) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   int e_head = 0;
-  if constexpr (FORM == kFormSplit) e_head = scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
+  if constexpr (FORM == kFormSplit) e_head = scale_exp(exp_of(top_of(a.tops, a.top_parts, lds)));
   for (int i = group * 4 + wave; i < a.count; i += groups * 4)
     pack_row<FORM, false>(a.head + (a.v0 + i) * a.head_row, a.v0 + i < a.V ? a.d : 0, a.width, 0, a.out + i * a.stride, a.plane, e_head,
                                 nullptr, 0, 0, lane);
@@ -514,7 +532,7 @@ struct HeadArgs {
   int64_t parts;
   float* at_target;
   const float* tops;
-  int top_parts[2];
+  int top_parts;
   // gradients
   Operand G;         // (p - y) of the piece [N, v] in 16 bits
   float* dh;         // [slices][rows][d] float32
@@ -576,28 +594,39 @@ EPIC_DEV void with_size(int size, F&& f) {
   f(t);
 }
 
-// What sums of products are multiplied with to be logits.
+// The head's power of two.
 template <int FORM>
-EPIC_DEV float unscale(const HeadArgs& a, float* lds) {
-  if constexpr (FORM != kFormSplit) return 1.f;
-  const int e = scale_exp(top_of(a.tops, a.top_parts[0], lds)) + scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
-  return __builtin_amdgcn_ldexpf(1.f, -e);
+EPIC_DEV int head_exp(const HeadArgs& a, float* lds) {
+  if constexpr (FORM != kFormSplit) return 0;
+  return scale_exp(exp_of(top_of(a.tops, a.top_parts, lds)));
+}
+
+// A row's sums without its and the head's power of two, which is taken out number by number:
+// as a factor it could leave float32 where the logits do not.
+template <int FORM, class T>
+EPIC_DEV void unscale(T& t, int i, int e) {
+  if constexpr (FORM == kFormSplit) {
+#pragma unroll
+    for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t.acc[i][j][k] = __builtin_amdgcn_ldexpf(t.acc[i][j][k], e);
+  }
 }
 
 constexpr float kFar = 16777216.f;  // of a logit in powers of two: it is rounded to whole numbers
 
 // Losses: a tile's columns to a maximum and a sum for every row, over the wavefronts of a
 // row of tiles by LDS, and the logit of the row's token.  exp2 takes one product
-// and sum: with c = log2(e) (and what unscales sums) t c is rounded to T, and the
+// and sum: with c = log2(e), t c is rounded to T, and the
 // sum of 2^(l c - T) is too large by the factor 2^(t c - T), which is taken out.  Past
 // 2^31 that factor can leave float32: from kFar on a term is 2^((l - t) c).
 // 2867 rows of 32768 tokens, width 2048, in bfloat16: 333 us, 1.16 PFLOP/s (the ends
 // of 32-step tiles take a tenth); 16 rows of 131072 tokens, width 4096: 180 us, bound
 // by reading the head at 6.0 TB/s.
 template <int FORM, class T>
-EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem, float2* part, int (&target)[2][256]) {
+EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, int e_head, char* smem, float2* part, int (&target)[2][256], int (&scale)[2][256]) {
   const int m = ceil_div(count, T::BM), n = ceil_div(a.v1 - a.v0, T::BN);
-  const float c = by * kLog2e;
+  constexpr float c = kLog2e;
   auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
   every_tile<kPairs<FORM>>(
       t, smem, [&](int i) { return dealt(i, m * n); },
@@ -613,6 +642,7 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
         for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
           const int at = tm * T::BM + r;
           target[k][r] = at < count ? a.kept.target[at] - a.v0 - tn * T::BN : -1;
+          if constexpr (FORM == kFormSplit) scale[k][r] = at < count ? -(a.kept.scale[at] + e_head) : 0;
         }
       },
       [&](int id, int k) {
@@ -623,6 +653,7 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
 #pragma unroll
         for (int i = 0; i < T::MT; ++i) {
           const int r = T::row(i, lane), y = target[k][r];
+          if constexpr (FORM == kFormSplit) unscale<FORM>(t, i, scale[k][r]);
           if (cols < T::BN) {
 #pragma unroll
             for (int j = 0; j < T::NT; ++j)
@@ -634,7 +665,7 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
             for (int j = 0; j < T::NT; ++j)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (T::col(j, lane) + e == y) a.at_target[tm * T::BM + r] = t.acc[i][j][e] * by;
+                if (T::col(j, lane) + e == y) a.at_target[tm * T::BM + r] = t.acc[i][j][e];
           }
           float top = -kInf;
 #pragma unroll
@@ -659,7 +690,7 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, float by, char* smem
           }
           sum += __shfl_xor(sum, 16);
           sum += __shfl_xor(sum, 32);
-          if (lane < 16) part[wn * T::BM + r] = make_float2(top * by, far ? sum : sum * __builtin_amdgcn_exp2f(-__builtin_fmaf(base, c, -tc)));
+          if (lane < 16) part[wn * T::BM + r] = make_float2(top, far ? sum : sum * __builtin_amdgcn_exp2f(-__builtin_fmaf(base, c, -tc)));
         }
         lds_barrier();
         for (int r = T::wave() * 64 + T::lane_now(); r < T::BM; r += T::kThreads) {
@@ -680,10 +711,9 @@ __global__ void __launch_bounds__(kProductThreads) lse_kernel(HeadArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[kProductLds];
   __shared__ float lds_top[kProductThreads / 64];
   __shared__ float2 part[4 * 256];
-  __shared__ int target[2][256];
-  const int count = *a.kept.count;
-  const float by = unscale<FORM>(a, lds_top);
-  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { lse_tiles<FORM>(a, t, count, by, smem, part, target); });
+  __shared__ int target[2][256], scale[2][256];
+  const int count = *a.kept.count, e_head = head_exp<FORM>(a, lds_top);
+  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { lse_tiles<FORM>(a, t, count, e_head, smem, part, target, scale); });
 }
 
 // Losses from the tiles' maxima and sums, one wavefront a row.
@@ -717,10 +747,11 @@ __global__ void __launch_bounds__(256) loss_kernel(HeadArgs a, float* loss, floa
 // of columns past the vocabulary are 0: the products that follow sum over them.
 // 8192 rows of 16384 tokens, width 4096, in bfloat16: 785 us, 1.40 PFLOP/s.
 template <int FORM, class T>
-EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* smem, int (&target)[2][256], float2 (&scale)[2][256]) {
+EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, int e_head, char* smem, int (&target)[2][256], float2 (&factor)[2][256],
+                           int (&scale)[2][256]) {
   constexpr float kScale = kScaled<FORM> ? 16384.f : 1.f;
   const int m = ceil_div(count, T::BM), n = ceil_div(a.v1 - a.v0, T::BN);
-  const float c = by * kLog2e;
+  constexpr float c = kLog2e;
   auto place = [&](int id, int& tm, int& tn) { tile_of(id, m, n, tm, tn); };
   every_tile<kPairs<FORM>>(
       t, smem, [&](int i) { return dealt(i, m * n); },
@@ -744,7 +775,8 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
             x.y = a.kept.mul[at] * kScale * __builtin_amdgcn_exp2f(-__builtin_fmaf(lse, kLog2e, -x.x));
           }
           target[k][r] = y;
-          scale[k][r] = x;
+          factor[k][r] = x;
+          if constexpr (FORM == kFormSplit) scale[k][r] = at < count ? -(a.kept.scale[at] + e_head) : 0;
         }
       },
       [&](int id, int k) {
@@ -755,7 +787,8 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
 #pragma unroll
         for (int i = 0; i < T::MT; ++i) {
           const int r = T::row(i, lane), at = tm * T::BM + r, y = target[k][r];
-          const float2 x = scale[k][r];
+          const float2 x = factor[k][r];
+          if constexpr (FORM == kFormSplit) unscale<FORM>(t, i, scale[k][r]);
           char* row = const_cast<char*>(a.G.data) + at * a.G.stride + kPacked<FORM> * (int64_t)(tn * T::BN);
           const bool far = __any(fabsf(x.x) >= kFar);
           const bool some = __any((unsigned)(y - wn * (T::BN / T::WN)) < (unsigned)(T::BN / T::WN));
@@ -769,14 +802,14 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, float by, char* s
               const float lse = at < count ? a.kept.lse[at] : 0.f, w = at < count ? a.kept.mul[at] * kScale : 0.f;
 #pragma unroll
               for (int f = 0; f < 4 * T::F; ++f)
-                g[f] = w * __builtin_amdgcn_exp2f((t.acc[i][j + f / 4][f & 3] * by - lse) * kLog2e);
+                g[f] = w * __builtin_amdgcn_exp2f((t.acc[i][j + f / 4][f & 3] - lse) * kLog2e);
             }
             const int c0 = T::col(j, lane);
             if (some && (unsigned)(y - c0) < (unsigned)(4 * T::F)) {  // 1 - p without what p = 1 rounds away
               float l = 0.f;
 #pragma unroll
               for (int f = 0; f < 4 * T::F; ++f) l = c0 + f == y ? t.acc[i][j + f / 4][f & 3] : l;
-              const float own = a.kept.mul[at] * kScale * expm1f(l * by - a.kept.lse[at]);
+              const float own = a.kept.mul[at] * kScale * expm1f(l - a.kept.lse[at]);
 #pragma unroll
               for (int f = 0; f < 4 * T::F; ++f) g[f] = c0 + f == y ? own : g[f];
             }
@@ -798,10 +831,10 @@ __global__ void __launch_bounds__(kProductThreads) excess_kernel(HeadArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[kProductLds];
   __shared__ float lds_top[kProductThreads / 64];
   __shared__ int target[2][256];
-  __shared__ float2 scale[2][256];  // lse in powers of two, and what 2^(l - lse) is multiplied with
-  const int count = *a.kept.count;
-  const float by = unscale<FORM>(a, lds_top);
-  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { excess_tiles<FORM>(a, t, count, by, smem, target, scale); });
+  __shared__ float2 factor[2][256];  // lse in powers of two, and what 2^(l - lse) is multiplied with
+  __shared__ int scale[2][256];
+  const int count = *a.kept.count, e_head = head_exp<FORM>(a, lds_top);
+  with_size<Sizes<kKind<FORM>, true, true>>(tile_size<kKind<FORM>>(count, a.piece), [&](auto& t) { excess_tiles<FORM>(a, t, count, e_head, smem, target, factor, scale); });
 }
 
 // ---- The two products with G, in one launch: the hidden states' gradient G W
@@ -957,8 +990,8 @@ __global__ void __launch_bounds__(kProductThreads) grad_kernel(HeadArgs a) {
   int e_h = 0, e_w = 0;  // what takes the scales out of the sums
   if constexpr (FORM == kFormF16) e_h = -14, e_w = a.kept.count[1] - 14;
   if constexpr (FORM == kFormSplit) {
-    e_h = -14 - scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds_top));
-    e_w = a.kept.count[1] - 14 - scale_exp(top_of(a.tops, a.top_parts[0], lds_top));
+    e_h = -14 - head_exp<FORM>(a, lds_top);
+    e_w = a.kept.count[1] - 15 - 14;  // rows are scaled to 2^15, by the largest of what they bring
   }
   int first_tiles = 0;
   if (a.grad_hidden) {
@@ -978,7 +1011,7 @@ __global__ void __launch_bounds__(256) scatter_kernel(HeadArgs a) {
   const int slices = split_of<kKind<FORM>>(a, *a.kept.count).slices;
   if (slices == 1) return;  // written already
   int e_head = 0;
-  if constexpr (FORM == kFormSplit) e_head = -scale_exp(top_of(a.tops + a.top_parts[0], a.top_parts[1], lds));
+  if constexpr (FORM == kFormSplit) e_head = -head_exp<FORM>(a, lds);
   const int at = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
   if (at >= *a.kept.count) return;
   const int r = a.kept.src[at], b = r / a.rows;
@@ -1197,7 +1230,7 @@ __global__ void __launch_bounds__(kProductThreads) logits_kernel(HeadArgs a) {
 // ------------------------------------------------------------ host side
 constexpr int64_t kMaxRows = 1 << 24;
 constexpr int kMaxWidth = 65536;
-constexpr int kTopParts = 2048;  // workgroups that look for a tensor's largest magnitude, at most
+constexpr int kTopParts = 2048;  // workgroups that look for largest magnitudes, of hidden states and of the head, at most
 
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -1219,7 +1252,7 @@ struct Layout {
   int64_t piece;         // tokens of a piece
   int max_slices;        // of a piece's tokens, in the hidden states' gradient
   int64_t parts;
-  int64_t counts, count, src, target, lse, mul, exp, tops, at_target, part, H, H2, W, G, dh, bytes;
+  int64_t counts, count, src, target, lse, mul, exp, scale, row_exp, tops, at_target, part, H, H2, W, G, dh, bytes;
 };
 
 // The products read a head in its place when its rows are vectors of 16 bytes.
@@ -1276,7 +1309,9 @@ Layout layout_of(const epic_rows_desc* hidden, const epic_rows_desc* head, bool 
   l.lse = take(4 * l.padded);
   l.mul = take(4 * l.padded);
   l.exp = take(4 * l.padded);
-  l.tops = take(8 * kTopParts);
+  l.scale = take(4 * l.padded);
+  l.row_exp = take(4 * l.padded);
+  l.tops = take(4 * kTopParts);
   l.at_target = take(4 * l.padded);
   const int64_t whole = es * planes * l.width;  // bytes of a packed row in all its planes
   l.H = take(l.padded * whole);
@@ -1319,7 +1354,7 @@ template <int FORM>
 PackArgs pack_args(const Call& c, int v0) {
   return {(const char*)c.head->data, c.head->row_stride * kSize<kDtype<FORM>>, c.head->rows, c.head->vocab, v0,
           (int)up(std::min<int64_t>(c.head->rows - v0, c.l.piece), 64), const_cast<char*>(c.a.W.data), c.a.W.stride, c.a.W.plane,
-          (int)c.l.width, c.a.tops, {c.a.top_parts[0], c.a.top_parts[1]}};
+          (int)c.l.width, c.a.tops, c.a.top_parts};
 }
 inline int pack_groups(const PackArgs& p) { return std::min(2048, (p.count + 3) / 4); }
 
@@ -1329,15 +1364,16 @@ void gather(Call& c) {
   const int groups = (int)std::max<int64_t>(1, (c.l.rows + c.g.per - 1) / c.g.per);
   PackArgs p{};
   int more = 0;
+  if constexpr (FORM == kFormSplit && MODE != kQuantize) {
+    const int row_groups = (int)std::min<int64_t>(kTopParts, (c.l.rows + 3) / 4);
+    TopArgs t{c.g, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops), row_groups};
+    hipLaunchKernelGGL(top_kernel, dim3(row_groups + c.a.top_parts), dim3(256), 0, c.stream, t);
+  }
   if (c.l.rows <= 1024)
     c.g.counts = nullptr;
   else
     hipLaunchKernelGGL(count_kernel, dim3((int)((c.l.rows + 255) / 256)), dim3(256), 0, c.stream, c.g);
   if constexpr (MODE != kQuantize) {
-    if (FORM == kFormSplit) {
-      TopArgs t{c.g, MODE == kBackward, (const char*)c.head->data, c.head->row_stride * 4, const_cast<float*>(c.a.tops)};
-      hipLaunchKernelGGL(top_kernel, dim3(c.g.top_parts[0] + c.g.top_parts[1]), dim3(256), 0, c.stream, t);
-    }
     if (!c.l.direct) {
       p = pack_args<FORM>(c, 0);
       more = pack_groups(p);
@@ -1366,7 +1402,7 @@ template <int FORM>
 void set_up(Call& c, char* ws) {
   const Layout& l = c.l;
   Kept kept{(int32_t*)(ws + l.count), (int32_t*)(ws + l.src), (int32_t*)(ws + l.target), (float*)(ws + l.lse), (float*)(ws + l.mul),
-            (int32_t*)(ws + l.exp)};
+            (int32_t*)(ws + l.exp), (int32_t*)(ws + l.scale)};
   constexpr int64_t es = kPacked<FORM>;
   const int64_t stride = es * l.width, plane = l.padded * stride;
   c.g.kept = c.a.kept = kept;
@@ -1375,9 +1411,9 @@ void set_up(Call& c, char* ws) {
   c.g.stride = stride;
   c.g.plane = plane;
   c.g.out2 = ws + l.H2;
-  c.g.tops = c.a.tops = (float*)(ws + l.tops);
-  c.g.top_parts[0] = c.a.top_parts[0] = (int)std::min<int64_t>(kTopParts, (l.rows + 3) / 4);
-  c.g.top_parts[1] = c.a.top_parts[1] = std::min(kTopParts, (c.head->rows + 3) / 4);
+  c.g.row_exp = FORM == kFormSplit ? (int32_t*)(ws + l.row_exp) : nullptr;
+  c.a.tops = (float*)(ws + l.tops);
+  c.a.top_parts = std::min(kTopParts, (c.head->rows + 3) / 4);
   c.a.H = {ws + l.H, stride, plane};
   c.a.H2 = {ws + l.H2, stride, plane};
   if (l.direct)
@@ -1589,7 +1625,7 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
   c.g.rows = hidden->rows;
   c.g.d = hidden->vocab;
   c.g.win = {d_seqs, d_start, n};
-  c.g.kept = {(int32_t*)(ws + l.count), (int32_t*)(ws + l.src), nullptr, nullptr, nullptr, nullptr};
+  c.g.kept = {(int32_t*)(ws + l.count), (int32_t*)(ws + l.src), nullptr, nullptr, nullptr, nullptr, nullptr};
   c.g.out = ws + l.H;
   c.g.stride = l.stride;
   c.g.scale = (float*)(ws + l.scale);

@@ -1,10 +1,15 @@
 """The operators between hidden states and logits at the ends of what their inputs
-may be: strides above the least, rows that add nothing, logits past 2^31.
+may be: strides above the least, rows that add nothing,
+logits past 2^31, rows and weights of very unlike size.
 
 Tolerances as in test_gpu_head (u32 = 2^-24), by row: a row's logits are off by
 (8 sqrt(d) u32 + 2^-22) of its largest sum A of terms' magnitudes, its lse by that, 2e-5 and,
 where it is large, the roundings of a float32 number of its size (lse's sum, the loss's
-difference: 4 u32 |lse| for both)."""
+difference: 4 u32 |lse| for both).  In grad_head a float32 row's hidden states are two
+float16 numbers whose half step is 2^-25, of rows scaled so that the largest
+product of weight and magnitude of a row (powers of two, each below twice its number) is
+2^15: with |G| <= 1 times its weight, 2^-38 of the largest such product for every row; G itself,
+2^14 at most, is off by 2^-39 of its row's weight where it is small."""
 import math
 
 import pytest
@@ -105,3 +110,81 @@ def test_logits_past_two_to_the_31(dtype, m, epic):  # noqa: F811
         + (2.0 ** -25 + 4 * m * float(c.weight.abs().max()) * 2.0 ** -25 if dtype == "float16" else 0.0)
     bad = ~((gw.double() - want_w).abs() <= 3 * u * size_w + 8 * math.sqrt(2 * m) * U32 * size_w + left) & (want_w.abs() < 0.9 * lim)
     assert not bool(bad.any())
+
+
+# ---------------------------------------------- rows of very unlike size
+
+
+def check_rows(epic, c, loss, lse):  # noqa: F811
+    """Every row's loss and gradient of hidden states, and the head's gradient, within
+    what is theirs."""
+    on = torch.from_numpy(c.on)
+    want = head_ref.loss(c.h, c.w, c.target, c.on, c.weight)
+    _, e = by_row(c, want[1])
+    assert bool(((lse.cpu() - want[1]).abs() <= e).all())
+    assert bool(((loss.cpu() - want[0]).abs() <= 2 * e)[on].all())
+    gh, gw = backward(epic, c, lse)
+    given = lse.cpu().double()
+    if c.weight is not None:  # (0 times what a rounded lse would leave)
+        given = torch.where(c.weight == 0, want[1], given)
+    _, _, want_h, want_w, size_h, size_w = head_ref.loss(c.h, c.w, c.target, c.on, c.weight, given)
+    h, w = c.h.double().clone(), c.w.double()
+    h[~on] = 0
+    weight = torch.ones((c.B, c.m), dtype=torch.float64) if c.weight is None else c.weight.double().abs()
+    p = torch.softmax(h @ w.t(), -1) * (weight * on)[..., None]
+    terms = c.B * c.m
+    bound_h = size_h * (2.0 ** -22 + 8 * math.sqrt(c.V) * U32) + 2 * e[..., None] * (p @ w.abs()) + want_h.abs() * U32 \
+        + 2.0 ** -38 * weight[..., None] * w.abs().max() * c.V + 1e-37
+    assert bool(((gh.double() - want_h).abs() <= bound_h)[on].all())
+    most = weight * h.abs().amax(-1) * on
+    flat, rows = p.reshape(terms, -1), h.abs().reshape(terms, -1)
+    bound_w = size_w * (2.0 ** -22 + 8 * math.sqrt(terms) * U32) + (2 * e.reshape(-1, 1) * flat).t() @ rows + want_w.abs() * U32 \
+        + (2.0 ** -38 * terms * float(most.max()) + 2.0 ** -38 * float(most.sum())) + 1e-37
+    bad = ~((gw.double() - want_w).abs() <= bound_w)
+    assert not bool(bad.any()), (float((gw.double() - want_w).abs().max()), float(bound_w.max()), int(bad.sum()))
+
+
+@pytest.mark.parametrize("m,V", [(60, 300), (600, 70)])
+def test_a_row_far_larger_than_the_others(m, V, epic):  # noqa: F811
+    """Of weight 0, so that the head's gradient is the others' too."""
+    c = Case("float32", 2, m, V, 96, share=1.0, seed=7)
+    c.target.clamp_(min=0)
+    c.on = head_ref.counted(2, m, c.seqs, None, c.target)
+    c.full_h[..., :96] = torch.randn((2, m, 96), generator=torch.Generator().manual_seed(8))
+    c.full_h[0, 7] *= 2.0 ** 40
+    c.full_h[1, 11] *= 2.0 ** -50
+    c.weight[0, 7] = 0
+    loss, lse = forward(epic, c)
+    check_rows(epic, c, loss, lse)
+
+
+@pytest.mark.parametrize("m", [90, 1100])
+def test_products_of_weights_and_rows(m, epic):  # noqa: F811
+    """Rows 2^k smaller of weights 2^k larger all count alike in the head's gradient."""
+    c = Case("float32", 1, m, 200, 96, share=1.0, seed=9)
+    c.target.clamp_(min=0)
+    c.on = head_ref.counted(1, m, c.seqs, None, c.target)
+    k = (torch.arange(m) % 41).float()
+    c.full_h[0, :, :96] = torch.randn((m, 96), generator=torch.Generator().manual_seed(10)) * torch.exp2(-k)[:, None]
+    c.weight[0] = torch.exp2(k) * (0.5 + torch.rand(m, generator=torch.Generator().manual_seed(11)))
+    loss, lse = forward(epic, c)
+    check_rows(epic, c, loss, lse)
+
+
+def test_scales_whose_product_is_past_float32(epic):  # noqa: F811
+    """A head of 2^100, rows of 2^-100, and one of 2^60 whose logits are infinite."""
+    c = Case("float32", 1, 90, 120, 96, share=1.0, seed=12)
+    c.target.clamp_(min=0)
+    c.on = head_ref.counted(1, 90, c.seqs, None, c.target)
+    c.full_w *= 2.0 ** 100
+    c.full_h[0, :, :96] = torch.randn((90, 96), generator=torch.Generator().manual_seed(13)) * 2.0 ** -100
+    small = c.full_h[0, 4].clone()
+    c.full_h[0, 4] *= 2.0 ** 80
+    c.full_h[0, 4] *= 2.0 ** 80
+    loss, lse = forward(epic, c)
+    assert bool(torch.isnan(loss[0, 4])) and int(torch.isfinite(loss).sum()) == 89
+    c.full_h[0, 4] = small
+    loss2, lse2 = forward(epic, c)
+    loss[0, 4], lse[0, 4] = loss2[0, 4], lse2[0, 4]
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
+    check_rows(epic, c, loss, lse)
