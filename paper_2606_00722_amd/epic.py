@@ -553,9 +553,13 @@ def logits_q8(hidden, seqs, q, scale, logits, workspace, start=None, stream=None
 
 
 def alloc_head_loss_workspace(hidden, head, backward=True):
-    """Device memory for head_loss_forward (and _backward) of tensors like these."""
+    """Device memory for head_loss_forward (and _backward) of tensors like these,
+    wherever they lie: the library reads a head at some addresses where it is, and
+    writes it out in the workspace at others."""
     rows, mat = _rows("hidden", hidden), _matrix("head", head, hidden.get_device())
-    n = int(_lib.epic_head_loss_workspace_bytes(ctypes.byref(rows), ctypes.byref(mat), int(bool(backward))))
+    n, at = 0, head.data_ptr() & ~15
+    for mat.data in (at, at + head.element_size()):
+        n = max(n, int(_lib.epic_head_loss_workspace_bytes(ctypes.byref(rows), ctypes.byref(mat), int(bool(backward)))))
     return _torch.empty(n + 256, dtype=_torch.uint8, device=hidden.device)
 
 

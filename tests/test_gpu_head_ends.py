@@ -1,6 +1,6 @@
 """The operators between hidden states and logits at the ends of what their inputs
 may be: strides above the least, rows that add nothing,
-logits past 2^31, rows and weights of very unlike size.
+logits past 2^31, rows and weights of very unlike size, heads at odd addresses.
 
 Tolerances as in test_gpu_head (u32 = 2^-24), by row: a row's logits are off by
 (8 sqrt(d) u32 + 2^-22) of its largest sum A of terms' magnitudes, its lse by that, 2e-5 and,
@@ -188,3 +188,34 @@ def test_scales_whose_product_is_past_float32(epic):  # noqa: F811
     loss[0, 4], lse[0, 4] = loss2[0, 4], lse2[0, 4]
     assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
     check_rows(epic, c, loss, lse)
+
+
+# ------------------------------------------------------ heads at odd addresses
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("rows", [20, 90])
+def test_workspace_for_a_head_at_any_address(dtype, rows, epic):  # noqa: F811
+    """A workspace made for tensors of these shapes, types and strides does for a head that
+    lies in the middle of a buffer."""
+    c = Case(dtype, 1, rows, 5000, 64, share=1.0, seed=16)
+    h, seqs, w, y, _, weight = c.on_gpu()
+    ws = epic.alloc_head_loss_workspace(h, w)
+    ws1 = epic.alloc_head_loss_workspace(h, w, backward=False)
+    flat = torch.zeros(5000 * 64 + 1, dtype=DT[dtype], device="cuda")
+    odd = flat[1:].view(5000, 64)
+    odd.copy_(w)
+    out = []
+    for head in (w, odd):
+        loss, lse = torch.empty((1, rows), device="cuda"), torch.empty((1, rows), device="cuda")
+        gh, gw = torch.empty_like(h), torch.empty_like(w)
+        epic.head_loss_forward(h, seqs, head, y, loss, lse, ws1)
+        epic.head_loss_backward(h, seqs, head, y, lse, weight, gh, gw, ws)
+        out.append((loss, lse, gh, gw))
+    if dtype != "float32":
+        assert all(torch.equal(a, b) for a, b in zip(*out))
+        return
+    # few float32 rows take other products
+    e = by_row(c, out[0][1].double().cpu())[1]
+    assert all(bool(((a - b).abs().cpu() <= 4 * e).all()) for a, b in list(zip(*out))[:2])
+    assert all(bool(((a - b).abs() <= 1e-5 * a.abs().max()).all()) for a, b in list(zip(*out))[2:])
