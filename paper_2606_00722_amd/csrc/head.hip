@@ -19,6 +19,8 @@ constexpr uint32_t kThreePairs = 0x014;  // planes (0, 1), (1, 0), (0, 0): small
 template <int FORM>
 constexpr int kPacked = FORM == kFormF32 ? 4 : 2;  // bytes of a number that products read
 template <int FORM>
+constexpr bool kPacks = FORM != kFormF32;  // some heads are written out
+template <int FORM>
 constexpr bool kScaled = FORM == kFormF16 || FORM == kFormSplit;  // numbers are brought into float16's range
 
 // ------------------------------------------------------- rows that count
@@ -501,7 +503,7 @@ __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a, PackArgs 
   __shared__ float lds_f[kGather / 64];
   if ((int)blockIdx.x < groups)
     gather_rows<FORM, MODE>(a, (int)blockIdx.x, lds_n, lds_own, lds_f);
-  else if constexpr (MODE != kQuantize)
+  else if constexpr (kPacks<FORM> && MODE != kQuantize)
     pack_rows<FORM>(p, (int)blockIdx.x - groups, (int)gridDim.x - groups, lds_f);
 }
 
@@ -1373,7 +1375,7 @@ void gather(Call& c) {
     c.g.counts = nullptr;
   else
     hipLaunchKernelGGL(count_kernel, dim3((int)((c.l.rows + 255) / 256)), dim3(256), 0, c.stream, c.g);
-  if constexpr (MODE != kQuantize) {
+  if constexpr (kPacks<FORM> && MODE != kQuantize) {
     if (!c.l.direct) {
       p = pack_args<FORM>(c, 0);
       more = pack_groups(p);
@@ -1391,9 +1393,11 @@ void piece(Call& c, int v0) {
   c.a.add = v0 > 0;
   if (c.l.direct) {
     c.a.W.data = (const char*)c.head->data + v0 * c.a.W.stride;
-  } else if (v0 > 0) {
-    const PackArgs p = pack_args<FORM>(c, v0);
-    hipLaunchKernelGGL(pack_kernel<FORM>, dim3(pack_groups(p)), dim3(256), 0, c.stream, p);
+  } else if constexpr (kPacks<FORM>) {
+    if (v0 > 0) {
+      const PackArgs p = pack_args<FORM>(c, v0);
+      hipLaunchKernelGGL(pack_kernel<FORM>, dim3(pack_groups(p)), dim3(256), 0, c.stream, p);
+    }
   }
 }
 
