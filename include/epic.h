@@ -496,7 +496,8 @@ epic_status epic_logits_q8(const epic_rows_desc* hidden, const int32_t* d_seqs, 
  * [batch*rows]) is at least 0.  Rows that do not count have loss 0, lse 0 and
  * gradient 0; their hidden states are not read.  A token >= the vocabulary gives
  * loss NaN, and the row adds nothing to the gradients.  NaN and infinities go
- * their way through the sums; an infinite logit gives NaN.
+ * their way through the sums, where 0 times an infinity is NaN; a logit of +infinity
+ * gives NaN, one of -infinity has probability 0.
  *
  * The gradients go by pieces of the vocabulary: a piece's logits are computed
  * again and set against the forward pass's lse, G is kept for one piece (256 MiB

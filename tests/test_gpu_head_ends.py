@@ -1,6 +1,7 @@
 """The operators between hidden states and logits at the ends of what their inputs
 may be: strides above the least, rows that add nothing,
-logits past 2^31, rows and weights of very unlike size, heads at odd addresses.
+logits past 2^31, rows and weights of very unlike size, heads at odd addresses, rows in
+another order, losses of many rows.
 
 Tolerances as in test_gpu_head (u32 = 2^-24), by row: a row's logits are off by
 (8 sqrt(d) u32 + 2^-22) of its largest sum A of terms' magnitudes, its lse by that, 2e-5 and,
@@ -112,6 +113,36 @@ def test_logits_past_two_to_the_31(dtype, m, epic):  # noqa: F811
     assert not bool(bad.any())
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_logit_of_minus_infinity(dtype, epic):  # noqa: F811
+    """Out of finite numbers: the token has probability 0, its own loss is infinite."""
+    m, V, d = 6, 300, 128
+    c = Case(dtype, 2, m, V, d, share=1.0, seed=19)
+    g = torch.Generator().manual_seed(20)
+    c.full_h[..., :d] = (1e25 * (1 + torch.rand((2, m, d), generator=g))).to(DT[dtype])
+    c.full_w[:, :d] = (1e-26 * torch.randn((V, d), generator=g)).to(DT[dtype])
+    c.full_w[5] = -1e25
+    c.target = torch.randint(6, V, (2, m), generator=g).to(torch.int32)
+    c.target[0, 2] = 5
+    c.on = head_ref.counted(2, m, c.seqs, None, c.target)
+    loss, lse = forward(epic, c)
+    want = head_ref.loss(c.h, c.w, c.target, c.on, c.weight)
+    c2 = c.w.clone()
+    c2[5] = 0  # (the bound is by the other tokens)
+    A = (c.h.double().abs() @ c2.double().abs().t()).amax(-1)
+    e = 8 * math.sqrt(d) * U32 * A + 2e-5 + 4 * U32 * want[1].abs()
+    assert float(loss[0, 2]) == math.inf
+    loss[0, 2] = want[0][0, 2] = 0
+    assert bool(((lse.cpu() - want[1]).abs() <= e).all()) and bool(((loss.cpu() - want[0]).abs() <= 2 * e).all())
+    gh, gw = backward(epic, c, lse)
+    assert bool(torch.isfinite(gh).all()) and bool(torch.isfinite(gw).all())
+    # its row alone has a gradient at the token
+    want_w = -c.weight[0, 2].double() * c.h[0, 2].double()
+    assert bool(((gw[5].double() - want_w).abs() <= 3 * torch.finfo(DT[dtype]).eps / 2 * want_w.abs()).all())
+    own = c.weight[0, 2].double() * -c.w[5].double()
+    assert bool(((gh[0, 2].double() - own).abs() <= 3 * torch.finfo(DT[dtype]).eps / 2 * own.abs()).all())
+
+
 # ---------------------------------------------- rows of very unlike size
 
 
@@ -219,3 +250,62 @@ def test_workspace_for_a_head_at_any_address(dtype, rows, epic):  # noqa: F811
     e = by_row(c, out[0][1].double().cpu())[1]
     assert all(bool(((a - b).abs().cpu() <= 4 * e).all()) for a, b in list(zip(*out))[:2])
     assert all(bool(((a - b).abs() <= 1e-5 * a.abs().max()).all()) for a, b in list(zip(*out))[2:])
+
+
+# ------------------------------------------------------ orders, many rows
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_sequences_closer_than_rows(dtype, epic):  # noqa: F811
+    """Tensors of [m, B, d] turned round give what others do."""
+    c = Case(dtype, 5, 40, 260, 72, share=0.7, seed=17)
+    h, seqs, w, y, _, weight = c.on_gpu()
+    B, m, V, d = c.B, c.m, c.V, c.d
+    turned = h.transpose(0, 1).contiguous().transpose(0, 1)
+    assert turned.stride(0) == d and turned.stride(1) == B * d
+    out = []
+    for x in (h, turned):
+        loss, lse = torch.empty((B, m), device="cuda"), torch.empty((B, m), device="cuda")
+        gh = torch.full((m, B, d), 7.0, dtype=DT[dtype], device="cuda").transpose(0, 1) if x is turned else torch.full_like(h, 7.0)
+        gw = torch.empty_like(w)
+        ws = epic.alloc_head_loss_workspace(x, w)
+        epic.head_loss_forward(x, seqs, w, y, loss, lse, ws)
+        epic.head_loss_backward(x, seqs, w, y, lse, weight, gh, gw, ws)
+        q, s = epic.alloc_q8(V, d)
+        epic.quantize(w, q, s)
+        logits = torch.full((m, B, V), 3.0, device="cuda").transpose(0, 1) if x is turned else torch.full((B, m, V), 3.0, device="cuda")
+        keep = torch.from_numpy(c.on).cuda()
+        z = torch.where(keep[..., None], x, torch.zeros((), dtype=x.dtype, device="cuda")) if x is h else \
+            torch.where(keep[..., None], x, torch.zeros((), dtype=x.dtype, device="cuda")).transpose(0, 1).contiguous().transpose(0, 1)
+        epic.logits_q8(z, seqs, q, s, logits, epic.alloc_logits_q8_workspace(z))
+        out.append((loss, lse, gh, gw, logits))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    assert bool((out[0][4] == 3).any()) and bool((out[0][4] != 3).any())
+    # and the gradient over hidden states that lie so
+    ws = epic.alloc_head_loss_workspace(turned, w)
+    gw = torch.empty_like(w)
+    epic.head_loss_backward(turned, seqs, w, y, out[0][1], weight, turned, gw, ws)
+    assert torch.equal(turned, out[0][2]) and torch.equal(gw, out[0][3])
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("size", [(4, 250, 20096, 256, 0.9), (4, 700, 20011, 264, 0.9), (9, 700, 26000, 72, 0.95), (3, 100, 4992, 1088, 1.0)], ids=str)
+def test_losses_of_many_rows(dtype, size, epic):  # noqa: F811
+    """Every size of tile, several pieces of the vocabulary; 0 in rows that do not count."""
+    B, m, V, d, share = size
+    c = Case(dtype, B, m, V, d, share=share, seed=18)
+    loss, lse = forward(epic, c)
+    on = torch.from_numpy(c.on).cuda()
+    h, w, y = cut_on(c)
+    l = h @ w.t()
+    want = torch.logsumexp(l, -1)
+    A = float((h.abs() @ w.abs().t()).max())
+    e = (8 * math.sqrt(d) * U32 + (2.0 ** -22 if dtype == "float32" else 0.0)) * A + 2e-5
+    assert float((lse[on] - want).abs().max()) <= e
+    assert float((loss[on] - (want - l.gather(1, y[:, None])[:, 0])).abs().max()) <= 2 * e
+    assert not bool(loss[~on].any()) and not bool(lse[~on].any())
+
+
+def cut_on(c):
+    on = torch.from_numpy(c.on)
+    return c.h[on].double().cuda(), c.w.double().cuda(), c.target[on].long().cuda()
