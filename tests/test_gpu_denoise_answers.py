@@ -61,3 +61,20 @@ def test_first_step():
     got = model.logits(seqs)[torch.from_numpy(on).to(dev)]
     want = head_ref.logits_q8(model.hidden.cpu(), model.q.cpu()[:, : model.head.shape[1]], model.scale.cpu(), on, torch.bfloat16)
     assert torch.equal(got.cpu(), want)
+
+
+def test_step_goes_against_the_gradient():
+    from paper_2606_00722_amd import denoise
+
+    dev = torch.device("cuda:0")
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(2)
+    B, n, V = 2, 20, 130
+    model = denoise.AnswerDenoiser(B, n, V, dev, gen)
+    seqs = torch.full((B, n), -1, dtype=torch.int32, device=dev)
+    target = torch.randint(0, V, (B, n), generator=gen, device=dev).to(torch.int32)
+    model.train_step(seqs, target, lr=0.25)
+    on = head_ref.counted(B, n, seqs.cpu().numpy(), None, target.cpu())
+    _, _, _, want, _, size = head_ref.loss(model.hidden.cpu(), torch.zeros_like(model.head).cpu(), target.cpu(), on)
+    assert bool(((model.w.cpu().double() + 0.25 * want).abs() <= 0.25 * (size * 2.0 ** -8 + want.abs() * 2.0 ** -8 + 1e-12)).all())
+    assert bool(model.w.any()) and torch.equal(model.head, model.w.to(torch.bfloat16))
