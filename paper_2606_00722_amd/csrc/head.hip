@@ -507,6 +507,9 @@ __global__ void __launch_bounds__(kGather) gather_kernel(GatherArgs a, PackArgs 
     pack_rows<FORM>(p, (int)blockIdx.x - groups, (int)gridDim.x - groups, lds_f);
 }
 
+// Bound by memory: 131072 rows of 4096 bfloat16 numbers 301 us (1.6 GB, 5.4 TB/s), of float32
+// 516 (5.2); wider rows are read twice: 32768 of 8192 in bfloat16 210 us, 3.9 TB/s of one
+// reading.
 template <int DT>
 __global__ void __launch_bounds__(256) quantize_kernel(const char* data, int64_t seq_stride, int64_t row_stride, int rows, int total,
                                                        int d, int8_t* q, int64_t stride, float* scale) {
@@ -569,7 +572,8 @@ constexpr int kProductThreads = 512, kProductLds = 131072, kCus = 256;
 
 EPIC_DEV int ceil_div(int a, int b) { return (a + b - 1) / b; }
 // 0 large, 1 mid, 2 few: of a result of m x n sums, `copies` times.  The rounds
-// that the CUs take, by what a round of each size costs.
+// that the CUs take, by what a round of each size costs (in bfloat16 products, as above;
+// the other types go by the same numbers).
 EPIC_DEV int tile_cost(int size) { return size == 0 ? 20 : size == 1 ? 9 : 6; }
 template <int KIND>
 EPIC_DEV int tile_size(int m, int n, int copies = 1) {
@@ -742,7 +746,11 @@ __global__ void __launch_bounds__(256) loss_kernel(HeadArgs a, float* loss, floa
   }
 }
 
-// (p - y) times the rows' weights, in 16 bits (two planes where inputs have 32).
+// (p - y) times the rows' weights, in 16 bits (two planes where inputs have 32): the
+// matrix units' products with 16-bit hidden states and head take no wider numbers, and
+// two planes would double them.  It is a second rounding beside the result's: bfloat16
+// gradients are off by 2.4e-3 of their norm where one rounding leaves 1.7e-3, float16 by
+// 3.3e-4 and 2.1e-4.
 // float16 has few small numbers, so there p is multiplied with 2^14 and the
 // weights are in [1/2, 1): 2^-24 of p = 1 is a normal number.  Numbers of rows past
 // the last, of rows without a token (which have hidden states 0 and weight 0) and
@@ -1266,10 +1274,11 @@ bool head_direct(const epic_rows_desc* head) {
 
 // Few float32 rows are multiplied as they are: finding the head's largest magnitude
 // and writing it out in two parts takes longer than slower products.  Losses and
-// gradients in us, so and in two parts: 64 rows, 32768 tokens of width 2048 95 + 421
-// and 285 + 510 (128 rows: 158 + 803 and 244 + 492), 128 rows with 64 that count, 512
-// tokens of width 128 45 and 56 (100 rows, 4096 tokens of width 1024: 48 + 90 and 43
-// + 73).
+// gradients in us, so and in two parts: 32768 tokens of width 2048, 64 rows 82 + 412
+// and 241 + 434, 128 rows 151 + 701 and 249 + 489.  Which is better near the bound goes
+// by the width too, by a few us: 128 rows over heads of 2^18, 2^19, 2^20 and 2^21
+// numbers of width 128 54, 55, 66, 78 and 61, 66, 76, 101 in all, of width 512 77, 80, 81,
+// 91 and 60, 69, 75, 84 (64 rows of width 2048, 2^19 numbers: 169 and 103).
 bool as_it_is(const epic_rows_desc* hidden, const epic_rows_desc* head) {
   const int64_t rows = (int64_t)hidden->batch * hidden->rows, size = (int64_t)head->rows * head->vocab;
   return hidden->dtype == EPIC_F32 && head_direct(head) && head->vocab % 64 == 0 && (rows <= 64 || (rows <= kFewRows && size <= 1 << 19));
