@@ -97,9 +97,9 @@ EPIC_DEV uint32_t pack_bf16(float a, float b) {
   return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
 }
 // A 32-bit number as the sum of two 16-bit ones.  With the largest magnitude (of a
-// row of hidden states, of the head) scaled to [2^14, 2^15), numbers down to 2^-17 of it keep 22 bits and
-// a sign (the second one's half step: 2^-24 of the number), smaller ones an
-// error of 2^-40 of the largest.
+// row of hidden states, of the head) scaled to [2^14, 2^15), numbers down to 2^-17
+// of it keep 22 bits and a sign (the second one's half step: 2^-24 of the number),
+// smaller ones an error of 2^-40 of the largest.
 EPIC_DEV void split_f16(float x, _Float16& a, _Float16& b) {
   a = (_Float16)x;
   const float r = x - (float)a;
@@ -420,8 +420,8 @@ EPIC_DEV void gather_rows(const GatherArgs& a, int group, int (&lds_n)[kGather /
   }
 }
 
-// The powers of two of the largest finite magnitudes: of every row of hidden states
-// that counts (the first workgroups), and of the head, a number for each of the others.
+// The largest finite magnitudes: of every row of hidden states that counts its power
+// of two (the first workgroups), and of the head one number for each of the others.
 struct TopArgs {
   GatherArgs g;
   const char* head;
@@ -623,9 +623,9 @@ constexpr float kFar = 16777216.f;  // of a logit in powers of two: it is rounde
 
 // Losses: a tile's columns to a maximum and a sum for every row, over the wavefronts of a
 // row of tiles by LDS, and the logit of the row's token.  exp2 takes one product
-// and sum: with c = log2(e), t c is rounded to T, and the
-// sum of 2^(l c - T) is too large by the factor 2^(t c - T), which is taken out.  Past
-// 2^31 that factor can leave float32: from kFar on a term is 2^((l - t) c).
+// and sum: with c = log2(e), t c is rounded to T, and the sum of 2^(l c - T) is too
+// large by the factor 2^(t c - T), which is taken out.  Past 2^31 that factor can
+// leave float32: from kFar on a term is 2^((l - t) c).
 // 2867 rows of 32768 tokens, width 2048, in bfloat16: 333 us, 1.16 PFLOP/s (the ends
 // of 32-step tiles take a tenth); 16 rows of 131072 tokens, width 4096: 180 us, bound
 // by reading the head at 6.0 TB/s.
@@ -681,13 +681,14 @@ EPIC_DEV void lse_tiles(const HeadArgs& a, T& t, int count, int e_head, char* sm
           top = fmaxf(top, __shfl_xor(top, 16));  // the four lanes of a row
           top = fmaxf(top, __shfl_xor(top, 32));
           const float base = top > -kInf ? top : 0.f, tc = base * c;
-          const bool far = __any(fabsf(tc) >= kFar);
+          const bool far = fabsf(tc) >= kFar;
           float sum = 0.f;
-          if (far) {
+          if (__any(far)) {  // (rows beside a far one as ever)
+            const float b0 = far ? base : 0.f, t0 = far ? 0.f : tc;
 #pragma unroll
             for (int j = 0; j < T::NT; ++j)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((t.acc[i][j][e] - base) * c);
+              for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j][e] - b0, c, -t0));
           } else {
 #pragma unroll
             for (int j = 0; j < T::NT; ++j)
@@ -800,7 +801,7 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, int e_head, char*
           const float2 x = factor[k][r];
           if constexpr (FORM == kFormSplit) unscale<FORM>(t, i, scale[k][r]);
           char* row = const_cast<char*>(a.G.data) + at * a.G.stride + kPacked<FORM> * (int64_t)(tn * T::BN);
-          const bool far = __any(fabsf(x.x) >= kFar);
+          const bool far = fabsf(x.x) >= kFar;
           const bool some = __any((unsigned)(y - wn * (T::BN / T::WN)) < (unsigned)(T::BN / T::WN));
 #pragma unroll
           for (int j = 0; j < T::NT; j += T::F) {
@@ -808,11 +809,11 @@ EPIC_DEV void excess_tiles(const HeadArgs& a, T& t, int count, int e_head, char*
 #pragma unroll
             for (int f = 0; f < 4 * T::F; ++f)
               g[f] = x.y * __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[i][j + f / 4][f & 3], c, -x.x));
-            if (far) {  // the factors' product could leave float32
+            if (__any(far)) {  // the factors' product could leave float32
               const float lse = at < count ? a.kept.lse[at] : 0.f, w = at < count ? a.kept.mul[at] * kScale : 0.f;
 #pragma unroll
               for (int f = 0; f < 4 * T::F; ++f)
-                g[f] = w * __builtin_amdgcn_exp2f((t.acc[i][j + f / 4][f & 3] - lse) * kLog2e);
+                g[f] = far ? w * __builtin_amdgcn_exp2f((t.acc[i][j + f / 4][f & 3] - lse) * kLog2e) : g[f];
             }
             const int c0 = T::col(j, lane);
             if (some && (unsigned)(y - c0) < (unsigned)(4 * T::F)) {  // 1 - p without what p = 1 rounds away

@@ -113,6 +113,29 @@ def test_logits_past_two_to_the_31(dtype, m, epic):  # noqa: F811
     assert not bool(bad.any())
 
 
+@pytest.mark.parametrize("dtype,m", [("bfloat16", 64), ("float16", 64), ("float32", 64), ("float32", 90)])
+def test_rows_beside_large_logits(dtype, m, epic):  # noqa: F811
+    """Their losses and gradients are those without the large ones, bit for bit."""
+    c = Case(dtype, 1, m, 300, 128, share=1.0, seed=21)
+    c.target.clamp_(min=0)
+    c.on = head_ref.counted(1, m, c.seqs, None, c.target)
+    g = torch.Generator().manual_seed(22)
+    c.full_h[..., :128] = torch.randn((1, m, 128), generator=g).to(DT[dtype])
+    c.full_h[..., 0] = 0.01
+    c.full_w[:, 0] = (4000 * torch.randn(300, generator=g)).to(DT[dtype])
+    loss, lse = forward(epic, c)
+    gh, _ = backward(epic, c, lse)
+    rest = torch.arange(m) % 9 != 4
+    for row in (~rest).nonzero()[:, 0].tolist():
+        c.full_h[0, row] *= 2.0 ** (9 if dtype == "float16" else 40)
+        c.full_h[0, row, 0] = 60000.0 if dtype == "float16" else 2.0 ** 40
+    loss2, lse2 = forward(epic, c)
+    gh2, _ = backward(epic, c, lse2)
+    assert float(lse2[0, ~rest].min()) > 2.0 ** (24 if dtype == "float16" else 31)
+    assert torch.equal(loss[0, rest], loss2[0, rest]) and torch.equal(lse[0, rest], lse2[0, rest])
+    assert torch.equal(gh[0, rest], gh2[0, rest])
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 def test_logit_of_minus_infinity(dtype, epic):  # noqa: F811
     """Out of finite numbers: the token has probability 0, its own loss is infinite."""
